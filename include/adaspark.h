@@ -359,6 +359,120 @@ int adaspark_ffn_sparse(const adaspark_shape *shape, const adaspark_ffn_dims *di
                         size_t workspace_bytes, void *stream);
 
 /*
+ * Attention over packed prompts: text turns of different lengths, one sequence behind the other without padding.  Sequence s
+ * has the queries [q_start[s], q_start[s+1]) of Q and the keys [k_start[s], k_start[s+1]) of K and V.  Token i of its n queries
+ * attends the keys j <= i + m - n of its m (causal != 0: the last query sees the last key; a follow-up turn's queries attend the
+ * history before them) or all m (causal == 0):
+ *   O = sum_j p_j v_j,  p = softmax(q.k_j / sqrt(head_dim))
+ * A row without keys (m == 0, or causal and i + m - n < 0) gets O = 0 and lse = -inf.
+ *   Q          in   bf16 [q_tokens][q_heads][head_dim], a token's q_stride elements behind the one before
+ *   K, V       in   bf16 [k_tokens][kv_heads][head_dim], likewise k_stride and v_stride: slices of one fused projection
+ *                   will do.  A stride of 0 stands for a contiguous tensor.
+ *   q_start, k_start  in  i32 [sequences+1], ascending, device memory; they may be the same array.  Rows of O (lse, dQ) before the first start
+ *                   and behind the last are left as they were, and so are those of dK and dV.  (Starts that descend or point outside
+ *                   give undefined values inside the outputs, never an access outside the tensors.)
+ *   O          out  bf16 [q_tokens][q_heads][head_dim], contiguous
+ *   lse        out  fp32 [q_tokens][q_heads] natural-log sum-exp of the scaled logits, or NULL
+ *   workspace       adaspark_prompt_workspace_bytes(ADASPARK_PROMPT_ATTN): 0 unless there are so few rows that each row's keys are
+ *                   shared out to several workgroups; may then be NULL
+ * Score products are exact in fp32 and the log-sum-exp is that of fp32 weights; the weights are rounded to bf16 (off by up to 2^-8 of each) for their
+ * products with V.  K and V of a sequence have to be finite: a row may multiply the V of a key that it does not attend by a weight of 0.
+ * Limits: head_dim in {64, 128}; q_tokens*q_heads and k_tokens*kv_heads < 2^31; strides multiples of 8 up to 2^22, and
+ * at least heads*head_dim (otherwise ADASPARK_EINVAL).
+ */
+typedef struct {
+    int32_t sequences;                    /* at least 1                                             */
+    int32_t q_tokens, k_tokens;           /* tokens of Q and of K, V; 0 is allowed                  */
+    int32_t q_heads, kv_heads, head_dim;  /* q_heads % kv_heads == 0                                */
+    int64_t q_stride, k_stride, v_stride; /* elements from a token to the next; 0: contiguous       */
+} adaspark_prompts;
+
+typedef enum {
+    ADASPARK_PROMPT_ATTN = 0,
+    ADASPARK_PROMPT_ATTN_BWD = 1
+} adaspark_prompt_call;
+
+int adaspark_prompt_workspace_bytes(const adaspark_prompts *prompts, int which_call /* adaspark_prompt_call */, int causal,
+                                    size_t *bytes);
+int adaspark_prompt_attn(const adaspark_prompts *prompts, const void *Q, const void *K, const void *V, const int32_t *q_start,
+                         const int32_t *k_start, int causal, void *O, float *lse, void *workspace, size_t workspace_bytes,
+                         void *stream);
+
+/*
+ * Its backward pass, with delta = dO.O per row:
+ *   dV_j = sum p_j dO,  dS_j = p_j (dO.v_j - delta),  dQ = sum_j dS_j k_j / sqrt(head_dim),  dK_j = sum dS_j q / sqrt(head_dim)
+ * (dK, dV summed over all rows and all query heads of the KV head's group).
+ *   O, lse     in   as adaspark_prompt_attn returned them;  dO  in  bf16 [q_tokens][q_heads][head_dim], contiguous
+ *   dQ         out  bf16 [q_tokens][q_heads][head_dim];  dK, dV  out  bf16 [k_tokens][kv_heads][head_dim], contiguous
+ *   workspace       adaspark_prompt_workspace_bytes(ADASPARK_PROMPT_ATTN_BWD)
+ * Every sum has a fixed order: the same call gives the same bits.  Rows without keys get dQ = 0, keys that no row attends dK = dV = 0.
+ * Q and dO of a sequence have to be finite, too.  Outputs must not overlap inputs or each other (ADASPARK_EINVAL).
+ */
+int adaspark_prompt_attn_bwd(const adaspark_prompts *prompts, const void *Q, const void *K, const void *V, const void *O,
+                             const float *lse, const void *dO, const int32_t *q_start, const int32_t *k_start, int causal,
+                             void *dQ, void *dK, void *dV, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A paged key/value cache, for answers: K and V each [pages][kv_heads][page_size][head_dim], position p of sequence s in page
+ * table[s][p / page_size] at p % page_size.  A table entry that is no page of the cache (-1, say), and positions beyond a table
+ * row, hold no token: nothing is written there, they are read as zero and attended by nobody.
+ * format ADASPARK_CACHE_BF16: values as they are.  ADASPARK_CACHE_E4M3: a byte each (4 exponent bits, 3 mantissa bits, up to 448,
+ * the OCP format), with a scale per token and KV head, fp32 [pages][kv_heads][page_size]: the row's largest magnitude / 448 (at least 2^-126; 0
+ * for a row of zeros); a code is the nearest value of the format to x / scale, and stands for code * scale.  A row that holds an
+ * infinity or a NaN has a NaN for its scale.
+ * Limits: page_size a power of two; table_pages*page_size <= 2^30; pages*page_size < 2^31; q_heads, kv_heads, head_dim as above,
+ * sequences*q_heads < 2^31 (the sequences of a decode step that share a KV head's keys with more than 16 query heads read them once per 16).
+ */
+typedef enum {
+    ADASPARK_CACHE_BF16 = 0,
+    ADASPARK_CACHE_E4M3 = 1
+} adaspark_cache_format;
+
+typedef struct {
+    int32_t sequences;                   /* rows of the table, at least 1                   */
+    int32_t pages, page_size;            /* of the cache                                    */
+    int32_t table_pages;                 /* entries of a table row                          */
+    int32_t q_heads, kv_heads, head_dim;
+    int32_t format;                      /* adaspark_cache_format                           */
+} adaspark_cache;
+
+/*
+ * Writes new tokens' keys and values into the cache: sequence s's new tokens [start[s], start[s+1]) of K and V take its last
+ * positions, lengths[s] - n .. lengths[s] - 1 (lengths count them already, as the other calls want them); a token whose position is
+ * below 0 or has no page is not written.  What the cache holds elsewhere stays.  A page that two sequences of the call write to ends up
+ * with either's tokens (pages shared by sequences are for reading).
+ *   K, V       in   bf16 [tokens][kv_heads][head_dim], strides as for prompts
+ *   start      in   i32 [sequences+1];  table  in  i32 [sequences][table_pages];  lengths  in  i32 [sequences]
+ *   K_cache, V_cache  in/out;  k_scale, v_scale  in/out, NULL in bf16
+ */
+int adaspark_cache_write(const adaspark_cache *cache, int32_t tokens, const void *K, int64_t k_stride, const void *V,
+                         int64_t v_stride, const int32_t *start, const int32_t *table, const int32_t *lengths, void *K_cache,
+                         void *V_cache, float *k_scale, float *v_scale, void *stream);
+
+/*
+ * Reads histories back: K and V rows [start[s], start[s+1]) are the positions 0, 1, ... of sequence s, as bf16 (codes times scale,
+ * rounded once; zero where there is no page).  The other rows of K and V are left as they were.  With start as k_start the result
+ * feeds adaspark_prompt_attn for a follow-up turn.
+ *   K, V       out  bf16 [tokens][kv_heads][head_dim], contiguous
+ */
+int adaspark_cache_read(const adaspark_cache *cache, int32_t tokens, const int32_t *start, const int32_t *table,
+                        const void *K_cache, const void *V_cache, const float *k_scale, const float *v_scale, void *K, void *V,
+                        void *stream);
+
+/*
+ * Attention of one new token of each sequence over its lengths[s] positions of the cache (its own among them; lengths beyond a table row
+ * are cut to it): the formula of adaspark_prompt_attn with one query per sequence.  A sequence without keys gets O = 0, lse = -inf.
+ *   Q          in   bf16 [sequences][q_heads][head_dim];  O  out  likewise;  lse  out  fp32 [sequences][q_heads], or NULL
+ *   workspace       adaspark_decode_workspace_bytes: partial results of sequences whose keys several workgroups share; 0 for
+ *                   many sequences, may then be NULL
+ * Positions that hold no token, and what lies in a page behind a sequence's length, may hold anything, NaN included.
+ */
+int adaspark_decode_workspace_bytes(const adaspark_cache *cache, size_t *bytes);
+int adaspark_decode_attn(const adaspark_cache *cache, const void *Q, const int32_t *table, const int32_t *lengths,
+                         const void *K_cache, const void *V_cache, const float *k_scale, const float *v_scale, void *O,
+                         float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Measurement probes (not part of the method: they exist so that a benchmark can state what this GPU sustains next
  * to the datasheet peaks its kernels are priced against).
  *   adaspark_probe_copy  a plain streaming copy of `bytes` bytes (a multiple of 16) from src to dst, device buffers

@@ -9,7 +9,9 @@ from __future__ import annotations
 
 import ctypes
 import os
+from contextlib import nullcontext
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -17,6 +19,7 @@ from .build import lib_path
 
 CALL_CUBE_POOL, CALL_CUBE_SELECT, CALL_SPARSE_ATTN, CALL_DENSE_ATTN, CALL_ATTN_BWD, CALL_CUBE_SELECT_SHARED = 0, 1, 2, 3, 4, 5
 CALL_SPARSE_ATTN_CSR = 6
+PROMPT_ATTN, PROMPT_ATTN_BWD = 0, 1  # adaspark_prompt_call
 ECAPACITY = -5  # ADASPARK_ECAPACITY: what a selection call leaves in its device status word on list overflow
 
 
@@ -64,6 +67,63 @@ class _CFfnDims(ctypes.Structure):
     _fields_ = [("d_model", ctypes.c_int32), ("d_ff", ctypes.c_int32)]
 
 
+class _CPrompts(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("sequences", "q_tokens", "k_tokens", "q_heads", "kv_heads", "head_dim")] + [
+        (n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")]
+
+
+@dataclass(frozen=True)
+class PromptShape:
+    """Packed prompts: mirror of ``adaspark_prompts`` but for the strides, which the calls take from the tensors."""
+
+    sequences: int
+    q_tokens: int
+    k_tokens: int
+    q_heads: int
+    kv_heads: int
+    head_dim: int
+
+    def _c(self, q_stride: int = 0, k_stride: int = 0, v_stride: int = 0) -> _CPrompts:
+        return _CPrompts(self.sequences, self.q_tokens, self.k_tokens, self.q_heads, self.kv_heads, self.head_dim,
+                         q_stride, k_stride, v_stride)
+
+
+class _CCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("sequences", "pages", "page_size", "table_pages", "q_heads", "kv_heads",
+                                              "head_dim", "format")]
+
+
+CACHE_FORMATS = {"bf16": 0, "e4m3": 1}  # adaspark_cache_format
+
+
+@dataclass(frozen=True)
+class CacheShape:
+    """Mirror of ``adaspark_cache``; ``format``: "bf16" or "e4m3"."""
+
+    sequences: int
+    pages: int
+    page_size: int
+    table_pages: int
+    q_heads: int
+    kv_heads: int
+    head_dim: int
+    format: str = "bf16"
+
+    def _c(self) -> _CCache:
+        return _CCache(self.sequences, self.pages, self.page_size, self.table_pages, self.q_heads, self.kv_heads,
+                       self.head_dim, CACHE_FORMATS.get(self.format, -1))
+
+
+class Cache(NamedTuple):
+    """The buffers of a paged cache: K and V [pages, kv_heads, page_size, head_dim], bf16 or float8_e4m3fn (uint8 will do), and
+    for the latter the scales, fp32 [pages, kv_heads, page_size]."""
+
+    K: torch.Tensor
+    V: torch.Tensor
+    k_scale: torch.Tensor | None = None
+    v_scale: torch.Tensor | None = None
+
+
 class AdasparkError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status
@@ -94,6 +154,13 @@ EXPORTS = (
     "adaspark_ffn_workspace_bytes",
     "adaspark_ffn_select",
     "adaspark_ffn_sparse",
+    "adaspark_prompt_workspace_bytes",
+    "adaspark_prompt_attn",
+    "adaspark_prompt_attn_bwd",
+    "adaspark_cache_write",
+    "adaspark_cache_read",
+    "adaspark_decode_workspace_bytes",
+    "adaspark_decode_attn",
     "adaspark_probe_copy",
     "adaspark_probe_mfma",
 )
@@ -144,6 +211,15 @@ def load():
         lib.adaspark_ffn_workspace_bytes.argtypes = [sp, dp, ctypes.POINTER(ctypes.c_size_t)]
         lib.adaspark_ffn_select.argtypes = [sp, dp, vp, ctypes.c_float, ctypes.c_float, vp, vp, vp, vp]
         lib.adaspark_ffn_sparse.argtypes = [sp, dp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        pp, cp = ctypes.POINTER(_CPrompts), ctypes.POINTER(_CCache)
+        size, i32, i64 = ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64
+        lib.adaspark_prompt_workspace_bytes.argtypes = [pp, ctypes.c_int, ctypes.c_int, ctypes.POINTER(size)]
+        lib.adaspark_prompt_attn.argtypes = [pp, vp, vp, vp, vp, vp, ctypes.c_int, vp, vp, vp, size, vp]
+        lib.adaspark_prompt_attn_bwd.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, vp, vp, vp, vp, size, vp]
+        lib.adaspark_cache_write.argtypes = [cp, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+        lib.adaspark_cache_read.argtypes = [cp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        lib.adaspark_decode_workspace_bytes.argtypes = [cp, ctypes.POINTER(size)]
+        lib.adaspark_decode_attn.argtypes = [cp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
         for name in EXPORTS:
             if name != "adaspark_status_string":
                 getattr(lib, name).restype = ctypes.c_int
@@ -475,6 +551,178 @@ def cube_select_shared(shape: Shape, Q: torch.Tensor, kbar: torch.Tensor, top_p:
         _dev(sel_mask, torch.int32, R * words, "sel_mask"), _dev(sel_count, torch.int32, R, "sel_count"),
         workspace.data_ptr(), workspace.numel(), _stream()), "adaspark_cube_select_shared")
     return sel_mask, sel_count
+
+
+# ---- packed prompts and the paged cache.  These calls run on the device of their tensors, whichever is the current one, on
+# torch's current stream of that device.
+
+
+def _same_device(first: torch.Tensor, *others):
+    """A context with the tensors' device as the current one; raises if they are not all on it."""
+    if not isinstance(first, torch.Tensor) or first.device.type != "cuda":
+        raise ValueError("expected GPU tensors (this package has no CPU path)")
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on different devices: {first.device} and {t.device}")
+    return nullcontext() if first.device.index == torch.cuda.current_device() else torch.cuda.device(first.device)
+
+
+def _rows(t: torch.Tensor, tokens: int, heads: int, head_dim: int, name: str) -> tuple[int, int]:
+    """(pointer, stride of a token) of a bf16 [tokens, heads, head_dim] whose tokens may lie apart."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError(f"{name} must be a GPU tensor (this package has no CPU path)")
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != (tokens, heads, head_dim):
+        raise ValueError(f"{name}: expected torch.bfloat16 {(tokens, heads, head_dim)}, got {t.dtype} {tuple(t.shape)}")
+    row = heads * head_dim
+    if tokens == 0 or t.is_contiguous():
+        return t.data_ptr(), 0
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim) or (tokens > 1 and t.stride(0) < row):
+        raise ValueError(f"{name}: the heads of a token have to lie one behind the other, got strides {t.stride()}")
+    return t.data_ptr(), t.stride(0) if tokens > 1 else 0
+
+
+def _optional(t, dtype, numel, name):
+    return None if t is None else _dev(t, dtype, numel, name)
+
+
+def prompt_workspace_bytes(shape: PromptShape, which_call: int, causal: bool = True) -> int:
+    n, cs = ctypes.c_size_t(0), shape._c()
+    _check(load().adaspark_prompt_workspace_bytes(ctypes.byref(cs), which_call, int(bool(causal)), ctypes.byref(n)),
+           "adaspark_prompt_workspace_bytes")
+    return n.value
+
+
+def _scratch(need: int, workspace, like: torch.Tensor):
+    """(keeps it alive, pointer, bytes) of the caller's workspace, or of one made here."""
+    if workspace is None:
+        if need == 0:
+            return None, None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+    return workspace, _dev(workspace, torch.uint8, workspace.numel(), "workspace"), workspace.numel()
+
+
+def prompt_attn(shape: PromptShape, Q, K, V, q_start, k_start=None, causal: bool = True, O=None, lse=None, workspace=None,
+                return_lse: bool = False):
+    """Attention over packed prompts -> O bf16 [q_tokens, Hq, D] (and lse fp32 [q_tokens, Hq]).  Sequence s: the queries
+    q_start[s] .. q_start[s+1] and the keys k_start[s] .. k_start[s+1] (int32 [sequences + 1]; k_start None: q_start); its
+    last query sees its last key.  Q, K, V may be slices of one tensor (heads of a token one behind the other).  Rows of O and
+    lse that belong to no sequence are left as they were."""
+    k_start = q_start if k_start is None else k_start
+    Tq, Tk, Hq, Hkv, D, n = shape.q_tokens, shape.k_tokens, shape.q_heads, shape.kv_heads, shape.head_dim, shape.sequences
+    q, k, v = _rows(Q, Tq, Hq, D, "Q"), _rows(K, Tk, Hkv, D, "K"), _rows(V, Tk, Hkv, D, "V")
+    with _same_device(Q, K, V, q_start, k_start, O, lse, workspace):
+        if O is None:
+            O = torch.empty((Tq, Hq, D), dtype=torch.bfloat16, device=Q.device)
+        if lse is None and return_lse:
+            lse = torch.empty((Tq, Hq), dtype=torch.float32, device=Q.device)
+        cs = shape._c(q[1], k[1], v[1])
+        ws, ws_ptr, ws_bytes = _scratch(prompt_workspace_bytes(shape, PROMPT_ATTN, causal), workspace, Q)
+        _check(load().adaspark_prompt_attn(
+            ctypes.byref(cs), q[0], k[0], v[0], _dev(q_start, torch.int32, n + 1, "q_start"),
+            _dev(k_start, torch.int32, n + 1, "k_start"), int(bool(causal)), _dev(O, torch.bfloat16, Tq * Hq * D, "O"),
+            _optional(lse, torch.float32, Tq * Hq, "lse"), ws_ptr, ws_bytes, _stream()), "adaspark_prompt_attn")
+    return (O, lse) if return_lse else O
+
+
+def prompt_attn_bwd(shape: PromptShape, Q, K, V, O, lse, dO, q_start, k_start=None, causal: bool = True, workspace=None,
+                    dQ=None, dK=None, dV=None):
+    """Backward of ``prompt_attn`` -> (dQ, dK, dV) bf16, contiguous."""
+    k_start = q_start if k_start is None else k_start
+    Tq, Tk, Hq, Hkv, D, n = shape.q_tokens, shape.k_tokens, shape.q_heads, shape.kv_heads, shape.head_dim, shape.sequences
+    q, k, v = _rows(Q, Tq, Hq, D, "Q"), _rows(K, Tk, Hkv, D, "K"), _rows(V, Tk, Hkv, D, "V")
+    with _same_device(Q, K, V, O, lse, dO, q_start, k_start, workspace, dQ, dK, dV):
+        new = lambda t, *size: torch.empty(size, dtype=torch.bfloat16, device=Q.device) if t is None else t  # noqa: E731
+        dQ, dK, dV = new(dQ, Tq, Hq, D), new(dK, Tk, Hkv, D), new(dV, Tk, Hkv, D)
+        cs = shape._c(q[1], k[1], v[1])
+        ws, ws_ptr, ws_bytes = _scratch(prompt_workspace_bytes(shape, PROMPT_ATTN_BWD, causal), workspace, Q)
+        _check(load().adaspark_prompt_attn_bwd(
+            ctypes.byref(cs), q[0], k[0], v[0], _dev(O, torch.bfloat16, Tq * Hq * D, "O"),
+            _dev(lse, torch.float32, Tq * Hq, "lse"), _dev(dO, torch.bfloat16, Tq * Hq * D, "dO"),
+            _dev(q_start, torch.int32, n + 1, "q_start"), _dev(k_start, torch.int32, n + 1, "k_start"), int(bool(causal)),
+            _dev(dQ, torch.bfloat16, Tq * Hq * D, "dQ"), _dev(dK, torch.bfloat16, Tk * Hkv * D, "dK"),
+            _dev(dV, torch.bfloat16, Tk * Hkv * D, "dV"), ws_ptr, ws_bytes, _stream()), "adaspark_prompt_attn_bwd")
+    return dQ, dK, dV
+
+
+def alloc_cache(shape: CacheShape, device="cuda") -> Cache:
+    """An empty cache: zeros."""
+    size = (shape.pages, shape.kv_heads, shape.page_size, shape.head_dim)
+    if shape.format == "bf16":
+        return Cache(*(torch.zeros(size, dtype=torch.bfloat16, device=device) for _ in range(2)))
+    codes = (torch.zeros(size, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2))
+    return Cache(*codes, *(torch.zeros(size[:3], dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def _cache_args(shape: CacheShape, cache: Cache, table) -> tuple:
+    """Pointers of the cache's buffers and of the page table."""
+    if shape.format not in CACHE_FORMATS:
+        raise ValueError(f"format: expected one of {tuple(CACHE_FORMATS)}, got {shape.format!r}")
+    tokens = shape.pages * shape.kv_heads * shape.page_size
+    if shape.format == "bf16":
+        if cache.k_scale is not None or cache.v_scale is not None:
+            raise ValueError("a bf16 cache has no scales")
+        held = [_dev(t, torch.bfloat16, tokens * shape.head_dim, n) for t, n in ((cache.K, "cache.K"), (cache.V, "cache.V"))] + [None, None]
+    else:
+        held = [_dev(t, torch.uint8 if isinstance(t, torch.Tensor) and t.dtype == torch.uint8 else torch.float8_e4m3fn,
+                     tokens * shape.head_dim, n) for t, n in ((cache.K, "cache.K"), (cache.V, "cache.V"))]
+        held += [_dev(cache.k_scale, torch.float32, tokens, "cache.k_scale"), _dev(cache.v_scale, torch.float32, tokens, "cache.v_scale")]
+    return held, _dev(table, torch.int32, shape.sequences * shape.table_pages, "table")
+
+
+def cache_write(shape: CacheShape, K, V, start, cache: Cache, table, lengths) -> None:
+    """The new tokens K, V (bf16 [tokens, Hkv, D], packed by start, int32 [sequences + 1]) take the last positions of their sequences:
+    lengths (int32 [sequences]) counts them already.  table int32 [sequences, table_pages]: the sequences' pages, -1 for none."""
+    tokens = K.shape[0]
+    k, v = _rows(K, tokens, shape.kv_heads, shape.head_dim, "K"), _rows(V, tokens, shape.kv_heads, shape.head_dim, "V")
+    with _same_device(K, V, start, table, lengths, *cache):
+        held, pages = _cache_args(shape, cache, table)
+        cs = shape._c()
+        _check(load().adaspark_cache_write(
+            ctypes.byref(cs), tokens, k[0], k[1], v[0], v[1], _dev(start, torch.int32, shape.sequences + 1, "start"), pages,
+            _dev(lengths, torch.int32, shape.sequences, "lengths"), *held, _stream()), "adaspark_cache_write")
+
+
+def cache_read(shape: CacheShape, cache: Cache, table, start, tokens: int, K=None, V=None):
+    """Histories read back -> (K, V) bf16 [tokens, Hkv, D]: rows start[s] .. start[s+1] are the positions 0, 1, ... of sequence s.
+    With start as k_start they feed ``prompt_attn``."""
+    size = (tokens, shape.kv_heads, shape.head_dim)
+    with _same_device(cache.K, cache.V, cache.k_scale, cache.v_scale, table, start, K, V):
+        held, pages = _cache_args(shape, cache, table)
+        if K is None:
+            K = torch.empty(size, dtype=torch.bfloat16, device=cache.K.device)
+        if V is None:
+            V = torch.empty(size, dtype=torch.bfloat16, device=cache.K.device)
+        n = tokens * shape.kv_heads * shape.head_dim
+        cs = shape._c()
+        _check(load().adaspark_cache_read(
+            ctypes.byref(cs), tokens, _dev(start, torch.int32, shape.sequences + 1, "start"), pages, *held,
+            _dev(K, torch.bfloat16, n, "K"), _dev(V, torch.bfloat16, n, "V"), _stream()), "adaspark_cache_read")
+    return K, V
+
+
+def decode_workspace_bytes(shape: CacheShape) -> int:
+    n, cs = ctypes.c_size_t(0), shape._c()
+    _check(load().adaspark_decode_workspace_bytes(ctypes.byref(cs), ctypes.byref(n)), "adaspark_decode_workspace_bytes")
+    return n.value
+
+
+def decode_attn(shape: CacheShape, Q, cache: Cache, table, lengths, O=None, lse=None, workspace=None, return_lse: bool = False):
+    """Attention of one new token of each sequence (Q bf16 [sequences, Hq, D]) over its first lengths[s] positions of the cache ->
+    O bf16 [sequences, Hq, D] (and lse fp32 [sequences, Hq])."""
+    rows, D = shape.sequences * shape.q_heads, shape.head_dim
+    with _same_device(Q, table, lengths, O, lse, workspace, *cache):
+        held, pages = _cache_args(shape, cache, table)
+        if O is None:
+            O = torch.empty((shape.sequences, shape.q_heads, D), dtype=torch.bfloat16, device=Q.device)
+        if lse is None and return_lse:
+            lse = torch.empty((shape.sequences, shape.q_heads), dtype=torch.float32, device=Q.device)
+        ws, ws_ptr, ws_bytes = _scratch(decode_workspace_bytes(shape), workspace, Q)
+        cs = shape._c()
+        _check(load().adaspark_decode_attn(
+            ctypes.byref(cs), _dev(Q, torch.bfloat16, rows * D, "Q"), pages, _dev(lengths, torch.int32, shape.sequences, "lengths"),
+            *held, _dev(O, torch.bfloat16, rows * D, "O"), _optional(lse, torch.float32, rows, "lse"), ws_ptr, ws_bytes,
+            _stream()), "adaspark_decode_attn")
+    return (O, lse) if return_lse else O
 
 
 def probe_copy(dst: torch.Tensor, src: torch.Tensor) -> int:

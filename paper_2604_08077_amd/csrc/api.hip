@@ -1,8 +1,12 @@
 // extern "C" boundary of the library: argument validation and kernel enqueueing only.
+#include <algorithm>
 #include <mutex>
+#include <utility>
 
 #include "geom.h"
 #include "ffn.h"
+#include "cache.h"
+#include "prompt.h"
 
 using namespace adaspark;
 
@@ -57,6 +61,55 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb)
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x < y + nb && y < x + na;
 }
+
+int check_heads(int q_heads, int kv_heads, int head_dim)
+{
+    if (q_heads <= 0 || kv_heads <= 0 || head_dim <= 0 || q_heads % kv_heads != 0) return ADASPARK_EINVAL;
+    return head_dim == 64 || head_dim == 128 ? ADASPARK_OK : ADASPARK_EUNSUPPORTED;
+}
+
+// elements from a token to the next, 0: contiguous
+int check_stride(int64_t stride, int heads, int head_dim)
+{
+    if (stride != 0 && (stride < (int64_t)heads * head_dim || stride % 8 != 0)) return ADASPARK_EINVAL;
+    return std::max<int64_t>(stride, (int64_t)heads * head_dim) <= (1 << 22) ? ADASPARK_OK : ADASPARK_EUNSUPPORTED;
+}
+
+int check_prompts(const adaspark_prompts *p)
+{
+    if (p == nullptr || p->sequences <= 0 || p->q_tokens < 0 || p->k_tokens < 0) return ADASPARK_EINVAL;
+    int rc = check_heads(p->q_heads, p->kv_heads, p->head_dim);
+    if (rc != ADASPARK_OK) return rc;
+    for (const auto &x : {std::make_pair(p->q_stride, p->q_heads), std::make_pair(p->k_stride, p->kv_heads), std::make_pair(p->v_stride, p->kv_heads)})
+        if ((rc = check_stride(x.first, x.second, p->head_dim)) != ADASPARK_OK) return rc;
+    if ((long long)p->q_tokens * p->q_heads >= (1ll << 31) || (long long)p->k_tokens * p->kv_heads >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
+    // the workgroups of a launch, with room for spans and parts
+    if (((long long)p->q_tokens * (p->q_heads / p->kv_heads) / 256 + p->sequences) * p->kv_heads >= (1ll << 24)) return ADASPARK_EUNSUPPORTED;
+    if (((long long)p->k_tokens / 256 + p->sequences) * p->kv_heads >= (1ll << 24)) return ADASPARK_EUNSUPPORTED;
+    return ADASPARK_OK;
+}
+
+int check_cache(const adaspark_cache *c)
+{
+    if (c == nullptr || c->sequences <= 0 || c->pages <= 0 || c->page_size <= 0 || c->table_pages <= 0) return ADASPARK_EINVAL;
+    if (c->format != ADASPARK_CACHE_BF16 && c->format != ADASPARK_CACHE_E4M3) return ADASPARK_EINVAL;
+    const int rc = check_heads(c->q_heads, c->kv_heads, c->head_dim);
+    if (rc != ADASPARK_OK) return rc;
+    if ((c->page_size & (c->page_size - 1)) != 0) return ADASPARK_EUNSUPPORTED;
+    if ((long long)c->table_pages * c->page_size > (1ll << 30) || (long long)c->pages * c->page_size >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
+    if ((long long)c->sequences * c->q_heads >= (1ll << 31) || c->q_heads >= (1 << 16)) return ADASPARK_EUNSUPPORTED;
+    return ADASPARK_OK;
+}
+
+// the cache's own buffers
+int check_cache_ptrs(const adaspark_cache *c, const void *K, const void *V, const float *ks, const float *vs)
+{
+    const int rc = check_ptrs({K, V});
+    if (rc != ADASPARK_OK) return rc;
+    return c->format == ADASPARK_CACHE_E4M3 ? check_ptrs({ks, vs}) : ks == nullptr && vs == nullptr ? ADASPARK_OK : ADASPARK_EINVAL;
+}
+
+bool aligned4(const void *p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 }  // namespace
 
@@ -470,6 +523,139 @@ int adaspark_ffn_sparse(const adaspark_shape *shape, const adaspark_ffn_dims *di
                                            static_cast<const uint16_t *>(W_gate), static_cast<const uint16_t *>(W_up),
                                            static_cast<const uint16_t *>(W_down), keep, static_cast<uint16_t *>(Y), w,
                                            static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ADASPARK_OK : ADASPARK_EHIP;
+}
+
+int adaspark_prompt_workspace_bytes(const adaspark_prompts *prompts, int which_call, int causal, size_t *bytes)
+{
+    if (bytes == nullptr) return ADASPARK_EINVAL;
+    const int rc = check_prompts(prompts);
+    if (rc != ADASPARK_OK) return rc;
+    const PromptGeom g = make_prompt_geom(*prompts, nullptr, nullptr, causal);
+    switch (which_call) {
+    case ADASPARK_PROMPT_ATTN: *bytes = prompt_workspace_bytes(g, prompts->head_dim); return ADASPARK_OK;
+    case ADASPARK_PROMPT_ATTN_BWD: *bytes = prompt_bwd_workspace_bytes(g, prompts->head_dim); return ADASPARK_OK;
+    default: return ADASPARK_EINVAL;
+    }
+}
+
+// a workspace of `need` bytes, which may be 0
+static int scratch_check(const void *workspace, size_t workspace_bytes, size_t need)
+{
+    if (need == 0) return ADASPARK_OK;
+    return workspace != nullptr && aligned16(workspace) && workspace_bytes >= need ? ADASPARK_OK : ADASPARK_EWORKSPACE;
+}
+
+int adaspark_prompt_attn(const adaspark_prompts *prompts, const void *Q, const void *K, const void *V, const int32_t *q_start,
+                         const int32_t *k_start, int causal, void *O, float *lse, void *workspace, size_t workspace_bytes,
+                         void *stream)
+{
+    int rc = check_prompts(prompts);
+    if (rc != ADASPARK_OK) return rc;
+    if (!aligned4(q_start) || !aligned4(k_start)) return ADASPARK_EINVAL;
+    const PromptGeom g = make_prompt_geom(*prompts, q_start, k_start, causal);
+    if (g.Tq > 0 && (rc = check_ptrs({Q, O})) != ADASPARK_OK) return rc;
+    if (g.Tk > 0 && (rc = check_ptrs({K, V})) != ADASPARK_OK) return rc;
+    if (lse != nullptr && !aligned16(lse)) return ADASPARK_EINVAL;
+    if ((rc = scratch_check(workspace, workspace_bytes, prompt_workspace_bytes(g, prompts->head_dim))) != ADASPARK_OK) return rc;
+    if (g.Tq == 0) return ADASPARK_OK;
+    const hipError_t e = launch_prompt_attn(g, prompts->head_dim, static_cast<const uint16_t *>(Q), static_cast<const uint16_t *>(K),
+                                            static_cast<const uint16_t *>(V), static_cast<uint16_t *>(O), lse, workspace,
+                                            static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ADASPARK_OK : ADASPARK_EHIP;
+}
+
+int adaspark_prompt_attn_bwd(const adaspark_prompts *prompts, const void *Q, const void *K, const void *V, const void *O,
+                             const float *lse, const void *dO, const int32_t *q_start, const int32_t *k_start, int causal, void *dQ,
+                             void *dK, void *dV, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_prompts(prompts);
+    if (rc != ADASPARK_OK) return rc;
+    if (!aligned4(q_start) || !aligned4(k_start)) return ADASPARK_EINVAL;
+    const PromptGeom g = make_prompt_geom(*prompts, q_start, k_start, causal);
+    const int D = prompts->head_dim;
+    if (g.Tq > 0 && (rc = check_ptrs({Q, O, lse, dO, dQ})) != ADASPARK_OK) return rc;
+    if (g.Tk > 0 && (rc = check_ptrs({K, V, dK, dV})) != ADASPARK_OK) return rc;
+    if ((rc = scratch_check(workspace, workspace_bytes, prompt_bwd_workspace_bytes(g, D))) != ADASPARK_OK) return rc;
+    auto extent = [&](int tokens, long long stride, int heads) { return tokens > 0 ? ((size_t)(tokens - 1) * stride + (size_t)heads * D) * 2 : 0; };
+    const size_t nq = (size_t)g.Tq * g.Hq * D * 2, nk = (size_t)g.Tk * g.Hkv * D * 2;
+    const std::pair<const void *, size_t> outs[3] = {{dQ, nq}, {dK, nk}, {dV, nk}};
+    const std::pair<const void *, size_t> ins[6] = {{Q, extent(g.Tq, g.qs, g.Hq)}, {K, extent(g.Tk, g.ks, g.Hkv)}, {V, extent(g.Tk, g.vs, g.Hkv)},
+                                                    {O, nq}, {dO, nq}, {lse, (size_t)g.Tq * g.Hq * 4}};
+    for (int a = 0; a < 3; ++a) {
+        for (const auto &in : ins)
+            if (outs[a].second && in.second && overlap(outs[a].first, outs[a].second, in.first, in.second)) return ADASPARK_EINVAL;
+        for (int b = 0; b < a; ++b)
+            if (outs[a].second && outs[b].second && overlap(outs[a].first, outs[a].second, outs[b].first, outs[b].second)) return ADASPARK_EINVAL;
+    }
+    if (g.Tq == 0 && g.Tk == 0) return ADASPARK_OK;
+    const hipError_t e = launch_prompt_bwd(g, D, static_cast<const uint16_t *>(Q), static_cast<const uint16_t *>(K),
+                                           static_cast<const uint16_t *>(V), static_cast<const uint16_t *>(O), lse,
+                                           static_cast<const uint16_t *>(dO), static_cast<uint16_t *>(dQ), static_cast<uint16_t *>(dK),
+                                           static_cast<uint16_t *>(dV), workspace, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ADASPARK_OK : ADASPARK_EHIP;
+}
+
+int adaspark_cache_write(const adaspark_cache *cache, int32_t tokens, const void *K, int64_t k_stride, const void *V, int64_t v_stride,
+                         const int32_t *start, const int32_t *table, const int32_t *lengths, void *K_cache, void *V_cache,
+                         float *k_scale, float *v_scale, void *stream)
+{
+    int rc = check_cache(cache);
+    if (rc != ADASPARK_OK) return rc;
+    if (tokens < 0 || !aligned4(start) || !aligned4(table) || !aligned4(lengths)) return ADASPARK_EINVAL;
+    if ((rc = check_cache_ptrs(cache, K_cache, V_cache, k_scale, v_scale)) != ADASPARK_OK) return rc;
+    if (tokens > 0 && (rc = check_ptrs({K, V})) != ADASPARK_OK) return rc;
+    if ((rc = check_stride(k_stride, cache->kv_heads, cache->head_dim)) != ADASPARK_OK) return rc;
+    if ((rc = check_stride(v_stride, cache->kv_heads, cache->head_dim)) != ADASPARK_OK) return rc;
+    if ((long long)tokens * cache->kv_heads >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
+    if (tokens == 0) return ADASPARK_OK;
+    const long long contiguous = (long long)cache->kv_heads * cache->head_dim;
+    const hipError_t e = launch_cache_write(make_cache_geom(*cache), tokens, static_cast<const uint16_t *>(K), k_stride ? k_stride : contiguous,
+                                            static_cast<const uint16_t *>(V), v_stride ? v_stride : contiguous, start, table, lengths,
+                                            CacheData{K_cache, V_cache, k_scale, v_scale}, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ADASPARK_OK : ADASPARK_EHIP;
+}
+
+int adaspark_cache_read(const adaspark_cache *cache, int32_t tokens, const int32_t *start, const int32_t *table, const void *K_cache,
+                        const void *V_cache, const float *k_scale, const float *v_scale, void *K, void *V, void *stream)
+{
+    int rc = check_cache(cache);
+    if (rc != ADASPARK_OK) return rc;
+    if (tokens < 0 || !aligned4(start) || !aligned4(table)) return ADASPARK_EINVAL;
+    if ((rc = check_cache_ptrs(cache, K_cache, V_cache, k_scale, v_scale)) != ADASPARK_OK) return rc;
+    if (tokens > 0 && (rc = check_ptrs({K, V})) != ADASPARK_OK) return rc;
+    if ((long long)tokens * cache->kv_heads >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
+    if (tokens == 0) return ADASPARK_OK;
+    const CacheData data{const_cast<void *>(K_cache), const_cast<void *>(V_cache), const_cast<float *>(k_scale), const_cast<float *>(v_scale)};
+    const hipError_t e = launch_cache_read(make_cache_geom(*cache), tokens, start, table, data, static_cast<uint16_t *>(K),
+                                           static_cast<uint16_t *>(V), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ADASPARK_OK : ADASPARK_EHIP;
+}
+
+int adaspark_decode_workspace_bytes(const adaspark_cache *cache, size_t *bytes)
+{
+    const int rc = check_cache(cache);
+    if (rc != ADASPARK_OK) return rc;
+    if (bytes == nullptr) return ADASPARK_EINVAL;
+    *bytes = decode_workspace_bytes(make_cache_geom(*cache));
+    return ADASPARK_OK;
+}
+
+int adaspark_decode_attn(const adaspark_cache *cache, const void *Q, const int32_t *table, const int32_t *lengths, const void *K_cache,
+                         const void *V_cache, const float *k_scale, const float *v_scale, void *O, float *lse, void *workspace,
+                         size_t workspace_bytes, void *stream)
+{
+    int rc = check_cache(cache);
+    if (rc != ADASPARK_OK) return rc;
+    if (!aligned4(table) || !aligned4(lengths)) return ADASPARK_EINVAL;
+    if ((rc = check_ptrs({Q, O})) != ADASPARK_OK) return rc;
+    if (lse != nullptr && !aligned16(lse)) return ADASPARK_EINVAL;
+    if ((rc = check_cache_ptrs(cache, K_cache, V_cache, k_scale, v_scale)) != ADASPARK_OK) return rc;
+    const CacheGeom g = make_cache_geom(*cache);
+    if ((rc = scratch_check(workspace, workspace_bytes, decode_workspace_bytes(g))) != ADASPARK_OK) return rc;
+    const CacheData data{const_cast<void *>(K_cache), const_cast<void *>(V_cache), const_cast<float *>(k_scale), const_cast<float *>(v_scale)};
+    const hipError_t e = launch_decode_attn(g, static_cast<const uint16_t *>(Q), table, lengths, data, static_cast<uint16_t *>(O), lse, workspace,
+                                            static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ADASPARK_OK : ADASPARK_EHIP;
 }
 

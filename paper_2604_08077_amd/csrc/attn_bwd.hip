@@ -26,7 +26,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "attn_tile.h"
+#include "rowtile.h"
 
 namespace adaspark {
 
@@ -128,45 +128,6 @@ BwdWorkspace bwd_workspace(const Geom &g, void *ws, bool in_place)
 
 size_t attn_bwd_workspace_bytes(const Geom &g) { return bwd_workspace(g, nullptr, false).bytes; }
 
-// Workgroup -> (KV head, slot among the head's workgroups).  Consecutive workgroups go to different XCDs, each with
-// its own L2; the workgroups of one KV head stream the same tiles, so where the head count allows a head's
-// workgroups stay on as few XCDs as possible.  bwd_grid is the matching launch size.
-__host__ __device__ inline bool bwd_head_slot(int b, int Hkv, int per_head, int &kv, int &slot)
-{
-    if (Hkv <= 8 && 8 % Hkv == 0) {
-        const int x = b & 7, idx = b >> 3, share = 8 / Hkv;
-        kv = x % Hkv;
-        slot = idx * share + x / Hkv;
-    } else if (Hkv % 8 == 0) {
-        const int x = b & 7, idx = b >> 3, m = Hkv / 8;
-        kv = x + 8 * (idx % m);
-        slot = idx / m;
-    } else {
-        kv = b % Hkv;
-        slot = b / Hkv;
-    }
-    return slot < per_head;
-}
-inline unsigned bwd_grid(int Hkv, int per_head)
-{
-    if (Hkv <= 8 && 8 % Hkv == 0) return (unsigned)((per_head + 8 / Hkv - 1) / (8 / Hkv) * 8);
-    return (unsigned)per_head * (unsigned)Hkv;
-}
-
-// Direct-to-LDS copies with an address per lane: lane l moves the 16 (4) bytes at src to lds_addr + 16 * l (4 * l).
-__device__ __forceinline__ void dma_lane16(uint32_t lds_addr, const void *src)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(src) : "memory", "m0");
-}
-__device__ __forceinline__ void dma_lane4(uint32_t lds_addr, const void *src)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_addr), "v"(src) : "memory", "m0");
-}
-
-__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
 __global__ __launch_bounds__(256) void bwd_copy_rows_kernel(long long pieces, const uint4 *__restrict__ Q,
                                                             const uint4 *__restrict__ dO, uint4 *__restrict__ Qc,
                                                             uint4 *__restrict__ dOc)
@@ -361,7 +322,7 @@ __global__ __launch_bounds__(BWD_THREADS) void attn_bwd_dq_kernel(Geom g, const 
     // alike, on a grid of 9 x 10 2,824, 2,178.)
     const int nrows = g.S * g.G;
     int kv, slot;
-    if (!bwd_head_slot(blockIdx.x, g.Hkv, (nrows - 1) / ROWS + 1, kv, slot)) return;
+    if (!head_slot(blockIdx.x, g.Hkv, (nrows - 1) / ROWS + 1, kv, slot)) return;
     const int row1 = nrows - slot * ROWS, row0 = max(0, row1 - ROWS), last = row1 - 1;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -903,44 +864,6 @@ struct Dkv {
     static_assert(BYTES <= 160 * 1024, "LDS of one CU");
 };
 
-// Slot of 16-byte chunk c of tile row r.  An LDS line is 16 slots: one row of head-dim 128, two of 64.  A ds_read_b128 of 64 lanes is served
-// 16 lanes at a time, lanes 0-3, 12-15, 20-27 first: with the chunk index equal in 0-15 and one higher in 16-31, the
-// lines' swizzle values must be distinct and those of rows 4..11 closed under ^ 1.  A transposing read is served 32
-// lanes at a time, 8 rows at two neighbouring chunks: their values must differ above bit 0 (measured: 241 bytes per
-// clock for both kinds; a plain row number gives 227 and 122).
-template <int D>
-__device__ __forceinline__ int row_swizzle(int r)
-{
-    if (D == 128) return (((r & 7) ^ (((r >> 3) & 1) << 2)) << 1) | ((r >> 3) & 1);
-    const int line = r >> 1;
-    return (((line & 3) ^ (((line >> 2) & 1) << 1)) << 1) | ((line >> 2) & 1);
-}
-template <int D>
-__device__ __forceinline__ int row_tile_off(int r, int c)
-{
-    if (D == 128) return r * 256 + ((c ^ row_swizzle<D>(r)) << 4);
-    return (r >> 1) * 256 + (((((r & 1) << 3) | c) ^ row_swizzle<D>(r)) << 4);
-}
-
-// LDS reads by address.
-template <typename T>
-__device__ __forceinline__ T lds_read(uint32_t addr)
-{
-    return *reinterpret_cast<const __attribute__((address_space(3))) T *>(addr);
-}
-// Two transposing reads, `step` bytes apart.  In each, lane (n16, q4) gets the elements at column n16 of the four
-// 16-element row pieces that lanes 16 q4 .. 16 q4 + 15 point to (lane 4 k + m of them: 8 bytes, elements 4 m .. 4 m + 3 of
-// row k).
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-__device__ __forceinline__ bf16x8 lds_read_tr2(uint32_t addr, int step)
-{
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>(addr));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>(addr + step));
-    return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
 // SHARED: cubes of up to 128 tokens (a workgroup then has at most four wavefronts' worth of keys).  Wavefronts w and w + 4 take the
 // same keys, and the first and the second half of every tile's rows; their sums are added through LDS at the end
 // (dkv_shared).
@@ -966,7 +889,7 @@ __global__ __launch_bounds__(BWD_THREADS) void attn_bwd_dkv_kernel(Geom g, const
     int *base = reinterpret_cast<int *>(smem + C::OFF_BASE);
 
     int kv, slot;
-    if (!bwd_head_slot(blockIdx.x, g.Hkv, (int)(cut.nkb * cut.parts), kv, slot)) return;
+    if (!head_slot(blockIdx.x, g.Hkv, (int)(cut.nkb * cut.parts), kv, slot)) return;
     const int kb = slot % cut.nkb;
     const int pidx = (int)cut.parts - 1 - slot / cut.nkb;  // the later ranges, which have the most parts, first
     int c = (int)((sqrtf(1.0f + 8.0f * (float)pidx / (float)cut.span) - 1.0f) * 0.5f);
@@ -1337,10 +1260,10 @@ static hipError_t launch_bwd_d(const Geom &g, const uint16_t *Q, const uint16_t 
     constexpr int TILE = 64 * D * 2;
 
     const int waves = bwd_dq_waves(g), keys = std::min(2, waves), rows_q = BWD_ROWS / keys;
-    const dim3 grid_q(bwd_grid(g.Hkv, (g.S * g.G - 1) / rows_q + 1));
+    const dim3 grid_q(head_grid(g.Hkv, (g.S * g.G - 1) / rows_q + 1));
     const int lds_q = 2 * 3 * TILE + BWD_ROWS * 16 + ADASPARK_MAX_CUBES / 8 + ADASPARK_MAX_CUBES * 2 + 16;
     const BwdParts &cut = w.cut;
-    const dim3 grid_k(bwd_grid(g.Hkv, (int)(cut.nkb * cut.parts)));
+    const dim3 grid_k(head_grid(g.Hkv, (int)(cut.nkb * cut.parts)));
     constexpr int lds_k = Dkv<D>::BYTES;
     auto launch_dq = [&](auto masked, auto keys_c, auto small) -> hipError_t {
         constexpr bool MASKED = decltype(masked)::value, SMALL = decltype(small)::value;

@@ -1,0 +1,205 @@
+// Writing new tokens' keys and values into the paged cache, and reading whole histories back (layout: cache.h).
+//
+// Both kernels give a row -- one token of one KV head, K and V -- to D / 8 lanes, 16 bytes of bf16 each, and find the row's
+// sequence by a binary search of the packed starts, which the workgroup holds in LDS.  Bound by HBM: every byte is read
+// once and written once.
+#include "cache.h"
+
+namespace adaspark {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int CACHE_THREADS = 256;
+constexpr int STARTS_LDS = 1024;  // starts held in LDS; with more sequences they are searched in memory
+
+// The sequence of token t: the last s with starts[s] <= t, -1 if t lies in none.  Whatever starts holds, the result is in
+// range and t lies between the sequence's starts.
+__device__ __forceinline__ int sequence_of(const int32_t *starts, int B, int t, int &first, int &end)
+{
+    int lo = 0, hi = B;  // starts[lo] <= t (if any is), the answer is in [lo, hi)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (starts[mid] <= t) lo = mid;
+        else hi = mid;
+    }
+    first = starts[lo];
+    end = starts[lo + 1];
+    return t >= first && t < end ? lo : -1;
+}
+
+__device__ __forceinline__ const int32_t *stage_starts(const int32_t *starts, int B, int32_t *lds)
+{
+    if (B >= STARTS_LDS) return starts;
+    for (int x = threadIdx.x; x <= B; x += CACHE_THREADS) lds[x] = starts[x];
+    __syncthreads();
+    return lds;
+}
+
+// Where position `pos` of sequence s lies: the token's index in its page's run and the page, or page -1.
+__device__ __forceinline__ int page_of(const CacheGeom &g, const int32_t *table, int s, int pos)
+{
+    if (pos < 0 || (pos >> g.shift) >= g.table_pages) return -1;
+    const int page = table[(size_t)s * g.table_pages + (pos >> g.shift)];
+    return (unsigned)page < (unsigned)g.pages ? page : -1;
+}
+__device__ __forceinline__ size_t cache_row(const CacheGeom &g, int page, int kv, int pos)
+{
+    return (((size_t)page * g.Hkv + kv) << g.shift) + (pos & ((1 << g.shift) - 1));
+}
+
+// e4m3 (4 exponent bits, 3 mantissa bits, up to 448) of one row: the scale is the row's largest magnitude over 448, at least
+// the smallest normal float, so that its reciprocal is finite; 0 for a row of zeros.  A row that holds an infinity or a NaN gets a
+// NaN for its scale: it reads back as NaN.
+template <int CPR>
+__device__ __forceinline__ uint2 quantise_row(uint4 x, float &scale)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t top = 0;  // of the magnitudes' bf16 bits: they order as the magnitudes do, infinities and NaN above
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
+#pragma unroll
+    for (int d = CPR / 2; d >= 1; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+    const float amax = __uint_as_float(top << 16);
+    scale = top == 0u ? 0.f : fmaxf(amax / 448.f, 1.17549435e-38f);
+    const float inv = top == 0u ? 0.f : 1.0f / scale;
+    if (top >= 0x7f80u) {
+        scale = __uint_as_float(0x7fc00000u);
+        return make_uint2(0u, 0u);
+    }
+    uint32_t q[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        int v = 0;
+        const auto value = [&](uint32_t bits) { return fminf(fmaxf(__uint_as_float(bits) * inv, -448.f), 448.f); };
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(value(w[2 * e] << 16), value(w[2 * e] & 0xffff0000u), v, false);
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(value(w[2 * e + 1] << 16), value(w[2 * e + 1] & 0xffff0000u), v, true);
+        q[e] = (uint32_t)v;
+    }
+    return make_uint2(q[0], q[1]);
+}
+
+// 8 codes times their scale, rounded to bf16 once.
+__device__ __forceinline__ uint4 values_of(uint2 q, float scale)
+{
+    uint32_t r[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t word = e < 2 ? q.x : q.y;
+        const bf16x2 c = e & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, 1.0f, true)
+                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, 1.0f, false);
+        r[e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)((float)c[0] * scale), (__bf16)((float)c[1] * scale)});
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+template <int D, bool E4M3>
+__global__ __launch_bounds__(CACHE_THREADS) void cache_write_kernel(CacheGeom g, int tokens, const uint16_t *__restrict__ K,
+                                                                    long long k_stride, const uint16_t *__restrict__ V,
+                                                                    long long v_stride, const int32_t *__restrict__ starts,
+                                                                    const int32_t *__restrict__ table,
+                                                                    const int32_t *__restrict__ lengths, CacheData c)
+{
+    constexpr int CPR = D / 8;
+    __shared__ int32_t held[STARTS_LDS];
+    const uint32_t row = blockIdx.x * (CACHE_THREADS / CPR) + threadIdx.x / CPR;
+    const int col = threadIdx.x % CPR;
+    const int t = (int)(row / (uint32_t)g.Hkv), kv = (int)(row - (uint32_t)t * (uint32_t)g.Hkv);
+    uint4 k = make_uint4(0, 0, 0, 0), v = k;
+    if (t < tokens) {  // asked for before the search
+        k = *reinterpret_cast<const uint4 *>(K + t * k_stride + kv * D + col * 8);
+        v = *reinterpret_cast<const uint4 *>(V + t * v_stride + kv * D + col * 8);
+    }
+    const int32_t *at = stage_starts(starts, g.B, held);
+    int first, end;
+    const int s = t < tokens ? sequence_of(at, g.B, t, first, end) : -1;
+    int page = -1, pos = 0;
+    if (s >= 0) {
+        pos = lengths[s] - (end - t);
+        page = page_of(g, table, s, pos);
+    }
+    if (E4M3) {
+        float ks, vs;
+        const uint2 kq = quantise_row<CPR>(k, ks), vq = quantise_row<CPR>(v, vs);
+        if (page < 0) return;
+        const size_t r = cache_row(g, page, kv, pos);
+        reinterpret_cast<uint2 *>(c.K)[r * CPR + col] = kq;
+        reinterpret_cast<uint2 *>(c.V)[r * CPR + col] = vq;
+        if (col == 0) {
+            c.ks[r] = ks;
+            c.vs[r] = vs;
+        }
+    } else {
+        if (page < 0) return;
+        const size_t r = cache_row(g, page, kv, pos);
+        reinterpret_cast<uint4 *>(c.K)[r * CPR + col] = k;
+        reinterpret_cast<uint4 *>(c.V)[r * CPR + col] = v;
+    }
+}
+
+template <int D, bool E4M3>
+__global__ __launch_bounds__(CACHE_THREADS) void cache_read_kernel(CacheGeom g, int tokens, const int32_t *__restrict__ starts,
+                                                                   const int32_t *__restrict__ table, CacheData c,
+                                                                   uint16_t *__restrict__ K, uint16_t *__restrict__ V)
+{
+    constexpr int CPR = D / 8;
+    __shared__ int32_t held[STARTS_LDS];
+    const int32_t *at = stage_starts(starts, g.B, held);
+    const uint32_t row = blockIdx.x * (CACHE_THREADS / CPR) + threadIdx.x / CPR;
+    const int col = threadIdx.x % CPR;
+    const int t = (int)(row / (uint32_t)g.Hkv), kv = (int)(row - (uint32_t)t * (uint32_t)g.Hkv);
+    if (t >= tokens) return;
+    int first, end;
+    const int s = sequence_of(at, g.B, t, first, end);
+    if (s < 0) return;
+    const int page = page_of(g, table, s, t - first);
+    uint4 k = make_uint4(0, 0, 0, 0), v = k;
+    if (page >= 0) {
+        const size_t r = cache_row(g, page, kv, t - first);
+        if (E4M3) {
+            k = values_of(reinterpret_cast<const uint2 *>(c.K)[r * CPR + col], c.ks[r]);
+            v = values_of(reinterpret_cast<const uint2 *>(c.V)[r * CPR + col], c.vs[r]);
+        } else {
+            k = reinterpret_cast<const uint4 *>(c.K)[r * CPR + col];
+            v = reinterpret_cast<const uint4 *>(c.V)[r * CPR + col];
+        }
+    }
+    reinterpret_cast<uint4 *>(K)[(size_t)row * CPR + col] = k;
+    reinterpret_cast<uint4 *>(V)[(size_t)row * CPR + col] = v;
+}
+
+template <typename F>
+static hipError_t by_kind(const CacheGeom &g, F &&launch)
+{
+    if (g.D == 64) g.e4m3 ? launch(std::integral_constant<int, 64>{}, std::true_type{})
+                          : launch(std::integral_constant<int, 64>{}, std::false_type{});
+    else g.e4m3 ? launch(std::integral_constant<int, 128>{}, std::true_type{})
+                : launch(std::integral_constant<int, 128>{}, std::false_type{});
+    return hipGetLastError();
+}
+
+static unsigned cache_blocks(const CacheGeom &g, int tokens)
+{
+    const long long per = CACHE_THREADS / (g.D / 8);
+    return (unsigned)(((long long)tokens * g.Hkv + per - 1) / per);
+}
+
+hipError_t launch_cache_write(const CacheGeom &g, int tokens, const uint16_t *K, long long k_stride, const uint16_t *V,
+                              long long v_stride, const int32_t *starts, const int32_t *table, const int32_t *lengths,
+                              const CacheData &c, hipStream_t st)
+{
+    return by_kind(g, [&](auto d, auto e4m3) {
+        hipLaunchKernelGGL((cache_write_kernel<decltype(d)::value, decltype(e4m3)::value>), dim3(cache_blocks(g, tokens)),
+                           dim3(CACHE_THREADS), 0, st, g, tokens, K, k_stride, V, v_stride, starts, table, lengths, c);
+    });
+}
+
+hipError_t launch_cache_read(const CacheGeom &g, int tokens, const int32_t *starts, const int32_t *table, const CacheData &c,
+                             uint16_t *K, uint16_t *V, hipStream_t st)
+{
+    return by_kind(g, [&](auto d, auto e4m3) {
+        hipLaunchKernelGGL((cache_read_kernel<decltype(d)::value, decltype(e4m3)::value>), dim3(cache_blocks(g, tokens)),
+                           dim3(CACHE_THREADS), 0, st, g, tokens, starts, table, c, K, V);
+    });
+}
+
+}  // namespace adaspark

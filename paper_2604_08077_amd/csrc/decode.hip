@@ -1,0 +1,500 @@
+// Attention of one new token of each sequence over the paged cache (layout: cache.h): o = sum_j p_j v_j, p = softmax(c q.k_j)
+// over the sequence's `length` keys, the new token's own among them.
+//
+// Every key and value is read once and meets the query heads of its KV head only, so the time is that of reading them from
+// HBM: 4 * G FLOP per byte of bf16, which leaves the matrix pipes nearly idle, and the wavefronts' one task is to keep
+// enough bytes in flight.  A workgroup takes a part of one sequence's keys for one KV head (decode_plan: parts of one
+// length over the whole batch, as many as fill the chip), its four wavefronts every fourth tile of 8 KB of keys and 8 KB of values.
+// A wavefront is by itself: two stages of LDS that only it fills and reads, direct-to-LDS loads of the next tile in flight
+// while it works this one, no barrier before the end, when the four partial results are put together.
+// Sequences of several parts leave them (fp32) in the workspace, and decode_join_kernel puts these together.
+//
+// The products are the attention kernels': S^T = K.Q^T and O^T += V^T.P^T with 16x16x32 MFMAs, a lane's column is one query
+// head (16 at a time; heads beyond the group repeat its last one).  V is read from LDS transposed.  In 8 bits the codes
+// become bf16 as they leave LDS (exactly), the key's scale multiplies the score and the value's scale the probability.
+#include "cache.h"
+#include "rowtile.h"
+
+namespace adaspark {
+
+typedef int s32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int DECODE_PLAN_SEQS = 512;  // sequences that a wavefront's lanes hold the lengths of, eight each
+constexpr int DECODE_CUS = 256;
+
+template <int D, bool E4M3>
+struct Decode {
+    static constexpr int WAVES = 4;
+    static constexpr int THREADS = 64 * WAVES;
+    static constexpr int ROW = D * (E4M3 ? 1 : 2);  // bytes of a key
+    static constexpr int KEYS = 8192 / ROW;         // of a tile: 32, 64 or 128
+    static constexpr int CPR = ROW / 16;            // 16-byte chunks of a row
+    static constexpr int RPI = 64 / CPR;            // rows of one direct-to-LDS instruction
+    static constexpr int NI = 8;                    // such instructions for 8 KB
+    static constexpr int OFF_V = 8192;
+    static constexpr int OFF_KS = 16384;            // scales of the keys, then of the values
+    static constexpr int STAGE = 16384 + (E4M3 ? 2 * KEYS * 4 : 0);
+    static constexpr int PAGES = (KEYS < 64 ? 64 : KEYS) * 4;  // the page of each key of a tile
+    static constexpr int WAVE_BYTES = 2 * STAGE + 2 * PAGES;
+    static constexpr int BYTES = WAVES * WAVE_BYTES;
+    static_assert(BYTES <= 160 * 1024, "LDS of one CU");
+    static_assert(16 * D * 4 + 256 <= WAVE_BYTES, "a wavefront's result takes the place of its stages");
+};
+
+// How a batch's keys are cut: into parts of `chunk` keys, the last of a sequence shorter, an empty sequence one part without
+// keys; at most `most` parts in all.  Every wavefront works this out by itself, from the lengths.
+struct DecodePart {
+    int s, part, parts;  // -1: the batch has no such part
+    int item0;           // number of the sequence's first part
+    int key0, key1;
+};
+__host__ __device__ inline int decode_unit(const CacheGeom &g) { return 4 * 8192 / (g.D * (g.e4m3 ? 1 : 2)); }
+
+// Parts that a KV head and 16 query heads of its group get: a workgroup each, whole rounds of the chip's CUs, at least two for
+// a sequence on average -- the parts have one length, and lengths differ.
+__host__ __device__ inline int decode_parts(const CacheGeom &g)
+{
+    const long long rows = (long long)g.Hkv * ((g.G + 15) / 16);
+    if (g.B > DECODE_PLAN_SEQS) return g.B;
+    const long long slots = (2 * g.B * rows + DECODE_CUS - 1) / DECODE_CUS * DECODE_CUS;
+    return (int)(slots / rows > g.B ? slots / rows : g.B);
+}
+
+__device__ __forceinline__ int cache_length(const CacheGeom &g, int len)
+{
+    const long long most = (long long)g.table_pages << g.shift;
+    return max(0, (int)min((long long)len, most));
+}
+
+__device__ __forceinline__ int wave_sum(int x)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
+    return x;
+}
+
+// chunk of the batch: the smallest multiple of `unit` with at most `most` parts (lengths: of sequence 64 * c + lane)
+__device__ __forceinline__ int decode_chunk(const int (&len)[DECODE_PLAN_SEQS / 64], int chunks, int B, int unit, int most)
+{
+    const int lane = threadIdx.x & 63;
+    int top = 0;
+    float total = 0.f;
+#pragma unroll
+    for (int c = 0; c < DECODE_PLAN_SEQS / 64; ++c)
+        if (c < chunks) {
+            top = max(top, len[c]);
+            total += (float)len[c];
+        }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        top = max(top, __shfl_xor(top, d, 64));
+        total += __shfl_xor(total, d, 64);
+    }
+    // ceil(top / unit) units always do (a part for each sequence); fewer than total / most never do
+    int lo = max(1, (int)(total / ((float)unit * (float)most) * 0.9999f)), hi = max(1, (top + unit - 1) / unit);
+    lo = min(lo, hi);
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1, chunk = mid * unit;
+        int n = 0;
+#pragma unroll
+        for (int c = 0; c < DECODE_PLAN_SEQS / 64; ++c)
+            if (c < chunks && 64 * c + lane < B) n += max(1, (len[c] + chunk - 1) / chunk);
+        if (wave_sum(n) <= most) hi = mid;
+        else lo = mid + 1;
+    }
+    return __builtin_amdgcn_readfirstlane(lo) * unit;
+}
+
+// Part number `item` of the batch (item >= 0), or with item < 0 all parts of sequence `seq`.
+__device__ __forceinline__ DecodePart decode_plan(const CacheGeom &g, const int32_t *lengths, int item, int seq)
+{
+    DecodePart p = {-1, 0, 1, 0, 0, 0};
+    const int lane = threadIdx.x & 63;
+    if (g.B > DECODE_PLAN_SEQS) {  // enough sequences to fill the chip: a part for each
+        p.s = item >= 0 ? item : seq;
+        p.item0 = p.s;
+        p.key1 = cache_length(g, lengths[p.s]);
+        return p;
+    }
+    int len[DECODE_PLAN_SEQS / 64];
+    const int chunks = (g.B + 63) >> 6;
+#pragma unroll
+    for (int c = 0; c < DECODE_PLAN_SEQS / 64; ++c) len[c] = c < chunks && 64 * c + lane < g.B ? cache_length(g, lengths[64 * c + lane]) : 0;
+    const int chunk = decode_chunk(len, chunks, g.B, decode_unit(g), decode_parts(g));
+    int base = 0;
+    for (int c = 0; c < chunks; ++c) {
+        int mine = 0;
+#pragma unroll
+        for (int k = 0; k < DECODE_PLAN_SEQS / 64; ++k)
+            if (k == c) mine = len[k];
+        const int n = 64 * c + lane < g.B ? max(1, (mine + chunk - 1) / chunk) : 0;
+        int incl = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int up = __shfl_up(incl, d, 64);
+            if (lane >= d) incl += up;
+        }
+        const bool here = item >= 0 ? n > 0 && item >= base + incl - n && item < base + incl : 64 * c + lane == seq;
+        const unsigned long long b = __ballot(here);
+        if (b != 0ull) {
+            const int src = __builtin_amdgcn_readfirstlane(__ffsll(b) - 1);
+            p.s = 64 * c + src;
+            p.parts = __builtin_amdgcn_readlane(n, src);
+            p.item0 = base + __builtin_amdgcn_readlane(incl, src) - p.parts;
+            p.part = item >= 0 ? item - p.item0 : 0;
+            const int m = __builtin_amdgcn_readlane(mine, src);
+            p.key0 = min(p.part * chunk, m);
+            p.key1 = p.key0 + min(chunk, m - p.key0);
+            return p;
+        }
+        base += __builtin_amdgcn_readlane(incl, 63);
+    }
+    return p;
+}
+
+// Slot of 16-byte chunk c of row r in a tile of rows of 64, 128 or 256 bytes (a line: 256 bytes).
+template <int ROW>
+__device__ __forceinline__ int decode_off(int r, int c)
+{
+    if (ROW == 64) return (r >> 2) * 256 + (((((r & 3) << 2) | c) ^ ((r >> 2) & 3)) << 4);
+    return row_tile_off<ROW / 2>(r, c);
+}
+// The chunk that lies in slot `l` (0 .. 15) of row r's line.
+template <int ROW>
+__device__ __forceinline__ int decode_chunk_at(int r, int l)
+{
+    if (ROW == 64) return (l ^ ((r >> 2) & 3)) & 3;
+    return (l ^ row_swizzle<ROW / 2>(r)) & (ROW / 16 - 1);
+}
+
+// 8 codes as bf16, exactly.
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t a, uint32_t b)
+{
+    const bf16x2 x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
+    const bf16x2 x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
+    return bf16x8{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
+}
+
+// A part's result: O unnormalised, fp32 [16 heads][D], then m and l (base 2) of each head.
+__host__ __device__ inline size_t decode_part_floats(int D) { return 16 * (size_t)D + 32; }
+
+template <int D, bool E4M3>
+__global__ __launch_bounds__(256) void decode_attn_kernel(CacheGeom g, const uint16_t *__restrict__ Q,
+                                                          const int32_t *__restrict__ table,
+                                                          const int32_t *__restrict__ lengths,
+                                                          const unsigned char *__restrict__ Kc,
+                                                          const unsigned char *__restrict__ Vc, const float *__restrict__ ks,
+                                                          const float *__restrict__ vs, uint16_t *__restrict__ O,
+                                                          float *__restrict__ lse, float *__restrict__ parts)
+{
+    using C = Decode<D, E4M3>;
+    constexpr int KEYS = C::KEYS, KG = KEYS / 16, KSTEPS = D / 32, DT = D / 16;
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    const int lane = threadIdx.x & 63, n16 = lane & 15, q4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    const int groups = (g.G + 15) / 16, heads = g.Hkv * groups;
+    const int item = (int)(blockIdx.x / (unsigned)heads), hh = (int)(blockIdx.x % (unsigned)heads);
+    const int kv = hh / groups, head0 = kv * g.G + hh % groups * 16, nheads = min(16, (kv + 1) * g.G - head0);
+    const DecodePart p = decode_plan(g, lengths, item, 0);
+    if (p.s < 0) return;
+
+    // Q operands: MFMA k index 8 q4 + e of step c is d = 32 c + 8 q4 + e; in 8 bits, where a lane reads 16 codes at a time for
+    // two steps, step 2 c + u has d = 64 c + 16 q4 + 8 u + e.
+    bf16x8 qf[KSTEPS];
+    {
+        const uint16_t *q = Q + ((size_t)p.s * g.Hq + head0 + min(n16, nheads - 1)) * D;
+#pragma unroll
+        for (int c = 0; c < KSTEPS; ++c)
+            qf[c] = *reinterpret_cast<const bf16x8 *>(q + (E4M3 ? 64 * (c >> 1) + 16 * q4 + 8 * (c & 1) : 32 * c + 8 * q4));
+    }
+
+    const int ntiles = (p.key1 - p.key0 + KEYS - 1) / KEYS;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem + (uint32_t)(wave * C::WAVE_BYTES));
+    const uint32_t pages0 = lds0 + 2 * C::STAGE;
+    const int32_t *trow = table + (size_t)p.s * g.table_pages;
+    const int in_page = (1 << g.shift) - 1;
+    // the table entries of a tile's keys (past the sequence's end: its last key's)
+    auto ask_pages = [&](int t, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < C::PAGES / 256; ++u) {
+            const int key = min(p.key0 + t * KEYS + ((u * 64 + lane) & (KEYS - 1)), p.key1 - 1);
+            dma_lane4(__builtin_amdgcn_readfirstlane(pages0 + (uint32_t)(buf * C::PAGES + u * 256)), trow + (key >> g.shift));
+        }
+    };
+    // a tile's rows (keys of no page are read from page 0, and zeroed before they are used)
+    auto ask_rows = [&](int t, int buf) __attribute__((always_inline)) {
+        const uint32_t st = lds0 + (uint32_t)(buf * C::STAGE);
+        auto place = [&](int r) -> size_t {
+            const int key = min(p.key0 + t * KEYS + r, p.key1 - 1);
+            const int page = lds_read<int>(pages0 + (uint32_t)(buf * C::PAGES + 4 * r));
+            return (((size_t)((unsigned)page < (unsigned)g.pages ? page : 0) * g.Hkv + kv) << g.shift) + (key & in_page);
+        };
+#pragma unroll
+        for (int u = 0; u < C::NI; ++u) {
+            const int r = u * C::RPI + lane / C::CPR;
+            const size_t off = place(r) * C::ROW + decode_chunk_at<C::ROW>(r, lane & 15) * 16;
+            dma_lane16(__builtin_amdgcn_readfirstlane(st + (uint32_t)(u * 1024)), Kc + off);
+            dma_lane16(__builtin_amdgcn_readfirstlane(st + (uint32_t)(C::OFF_V + u * 1024)), Vc + off);
+        }
+        if (E4M3) {
+#pragma unroll
+            for (int u = 0; u < KEYS / 64; ++u) {
+                const size_t off = place(u * 64 + lane);
+                dma_lane4(__builtin_amdgcn_readfirstlane(st + (uint32_t)(C::OFF_KS + u * 256)), ks + off);
+                dma_lane4(__builtin_amdgcn_readfirstlane(st + (uint32_t)(C::OFF_KS + KEYS * 4 + u * 256)), vs + off);
+            }
+        }
+    };
+    auto wait_all = []() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
+
+    const float c2 = 1.44269504088896340736f / sqrtf((float)D);  // softmax scale in base 2
+    float m_run = -INFINITY, l_run = 0.f;  // of the lane's head; l: of the lane's keys only, until the end
+    f32x4 oacc[DT];
+#pragma unroll
+    for (int e = 0; e < DT; ++e) oacc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    int buf = 0;
+    if (wave < ntiles) {
+        ask_pages(wave, 0);
+        wait_all();
+        if (wave + C::WAVES < ntiles) ask_pages(wave + C::WAVES, 1);
+        ask_rows(wave, 0);
+    }
+    for (int t = wave; t < ntiles; t += C::WAVES, buf ^= 1) {
+        wait_all();  // this tile's rows and the next one's pages are there, and nobody reads the other stage any more
+        const int next = t + C::WAVES;
+        // Which of this tile's keys there are, before their table entries make room for those of the tile after the next.
+        bool whole = true;
+        unsigned long long there[(KEYS + 63) / 64];
+#pragma unroll
+        for (int u = 0; u < (KEYS + 63) / 64; ++u) {
+            const int r = u * 64 + (lane & (KEYS - 1));
+            const int page = lds_read<int>(pages0 + (uint32_t)(buf * C::PAGES + 4 * r));
+            there[u] = __ballot(p.key0 + t * KEYS + r < p.key1 && (unsigned)page < (unsigned)g.pages);
+            whole = whole && there[u] == ~0ull;
+        }
+        if (next < ntiles) {
+            if (next + C::WAVES < ntiles) ask_pages(next + C::WAVES, buf);
+            ask_rows(next, buf ^ 1);
+        }
+        const uint32_t st = lds0 + (uint32_t)(buf * C::STAGE);
+        if (!whole) {  // rows that are not there: values (and their scales) of zero, so that a probability of zero adds nothing
+            for (int r = 0; r < KEYS; ++r)
+                if (!((there[r >> 6] >> (r & 63)) & 1ull)) {
+                    if (lane < C::CPR)
+                        *reinterpret_cast<__attribute__((address_space(3))) u32x4 *>(st + C::OFF_V + decode_off<C::ROW>(r, lane)) =
+                            u32x4{0u, 0u, 0u, 0u};
+                    if (E4M3 && lane == 0)
+                        *reinterpret_cast<__attribute__((address_space(3))) float *>(st + C::OFF_KS + KEYS * 4 + 4 * r) = 0.f;
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+
+        f32x4 sacc[KG];
+#pragma unroll
+        for (int kg = 0; kg < KG; ++kg) {
+            sacc[kg] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (E4M3) {
+#pragma unroll
+                for (int c = 0; c < KSTEPS / 2; ++c) {
+                    const u32x4 k = lds_read<u32x4>(st + (uint32_t)decode_off<C::ROW>(16 * kg + n16, 4 * c + q4));
+                    sacc[kg] = mfma16(codes_to_bf16(k[0], k[1]), qf[2 * c], sacc[kg]);
+                    sacc[kg] = mfma16(codes_to_bf16(k[2], k[3]), qf[2 * c + 1], sacc[kg]);
+                }
+                const f32x4 scale = lds_read<f32x4>(st + (uint32_t)(C::OFF_KS + 4 * (16 * kg + 4 * q4)));
+                sacc[kg] *= scale;
+            } else {
+#pragma unroll
+                for (int c = 0; c < KSTEPS; ++c)
+                    sacc[kg] = mfma16(lds_read<bf16x8>(st + (uint32_t)decode_off<C::ROW>(16 * kg + n16, 4 * c + q4)), qf[c], sacc[kg]);
+            }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int kg = 0; kg < KG; ++kg)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const int r = 16 * kg + 4 * q4 + v;
+                    if (!((there[kg >> 2] >> (r & 63)) & 1ull)) sacc[kg][v] = -INFINITY;
+                }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kg = 0; kg < KG; ++kg) mx = vmax(vmax3(mx, sacc[kg][0], sacc[kg][1]), vmax(sacc[kg][2], sacc[kg][3]));
+        mx = quad_max(mx) * c2;
+        const float m_new = vmax(m_run, mx);
+        if (__ballot(m_new != m_run) != 0ull) {
+            const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);  // (no key so far: O and l are 0)
+#pragma unroll
+            for (int e = 0; e < DT; ++e) oacc[e] *= alpha;
+            l_run *= alpha;
+            m_run = m_new;
+        }
+        const float m_sub = m_run == -INFINITY ? 0.f : m_run;
+        bf16x8 pf[KEYS / 32];
+#pragma unroll
+        for (int kg = 0; kg < KG; ++kg) {
+            f32x4 w;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                w[v] = __builtin_amdgcn_exp2f(fmaf(sacc[kg][v], c2, -m_sub));
+                l_run += w[v];
+            }
+            if (E4M3) w *= lds_read<f32x4>(st + (uint32_t)(C::OFF_KS + KEYS * 4 + 4 * (16 * kg + 4 * q4)));
+            // P.V takes bf16 operands: a weight is off by up to 2^-8 of itself, as in the other attention kernels
+#pragma unroll
+            for (int v = 0; v < 4; ++v) pf[kg >> 1][4 * (kg & 1) + v] = (__bf16)w[v];
+        }
+        // O^T += V^T.P^T: MFMA k index 8 q4 + 4 x + v is key 32 sl + 16 x + 4 q4 + v
+#pragma unroll
+        for (int sl = 0; sl < KEYS / 32; ++sl)
+#pragma unroll
+            for (int e = 0; e < DT; ++e) {
+                bf16x8 vt;
+                if (E4M3) {
+                    typedef __attribute__((address_space(3))) s32x2 lds_s32x2;
+                    const int j = n16 >> 1, r = 32 * sl + 4 * q4 + (j & 3) + 16 * (j >> 2);
+                    const s32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<lds_s32x2 *>(
+                        st + (uint32_t)(C::OFF_V + decode_off<C::ROW>(r, e) + 8 * (n16 & 1))));
+                    vt = codes_to_bf16((uint32_t)x[0], (uint32_t)x[1]);
+                } else {
+                    const int r = 32 * sl + 4 * q4 + (n16 >> 2);
+                    vt = lds_read_tr2(st + (uint32_t)(C::OFF_V + decode_off<C::ROW>(r, 2 * e + ((n16 & 3) >> 1)) + 8 * (n16 & 1)),
+                                      16 * C::ROW);
+                }
+                oacc[e] = mfma16(vt, pf[sl], oacc[e]);
+            }
+    }
+    wait_all();
+
+    // ---- the wavefronts' results together: O = sum_w 2^(m_w - M) O_w.  A wavefront's lies where its stages were.
+    float *mine = reinterpret_cast<float *>(smem + wave * C::WAVE_BYTES);
+    l_run = quad_sum(l_run);
+#pragma unroll
+    for (int e = 0; e < DT; ++e) *reinterpret_cast<f32x4 *>(mine + n16 * D + 16 * e + 4 * q4) = oacc[e];
+    if (q4 == 0) {
+        mine[16 * D + n16] = m_run;
+        mine[16 * D + 16 + n16] = l_run;
+    }
+    __syncthreads();
+    float *out = p.parts > 1 ? parts + ((size_t)item * heads + hh) * decode_part_floats(D) : nullptr;
+    for (int x = threadIdx.x; x < nheads * (D / 4); x += C::THREADS) {
+        const int a = x / (D / 4), d = x % (D / 4) * 4;
+        float M = -INFINITY, L = 0.f, f[C::WAVES];
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < C::WAVES; ++w) M = fmaxf(M, reinterpret_cast<const float *>(smem + w * C::WAVE_BYTES)[16 * D + a]);
+#pragma unroll
+        for (int w = 0; w < C::WAVES; ++w) {
+            const float *from = reinterpret_cast<const float *>(smem + w * C::WAVE_BYTES);
+            f[w] = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(from[16 * D + a] - M);
+            L = fmaf(f[w], from[16 * D + 16 + a], L);
+            o += f[w] * *reinterpret_cast<const f32x4 *>(from + a * D + d);
+        }
+        if (out != nullptr) {
+            *reinterpret_cast<f32x4 *>(out + a * D + d) = o;
+            if (d == 0) {
+                out[16 * D + a] = M;
+                out[16 * D + 16 + a] = L;
+            }
+        } else {
+            const size_t row = (size_t)p.s * g.Hq + head0 + a;
+            *reinterpret_cast<uint2 *>(O + row * D + d) = pack_bf16(o * (L > 0.f ? 1.0f / L : 0.f));  // (no key: zero)
+            if (d == 0 && lse != nullptr) lse[row] = (M + log2f(L)) * 0.69314718055994530942f;
+        }
+    }
+}
+
+// The parts of a sequence put together, a wavefront for each (sequence, query head): lane l has D / 64 columns.
+template <int D>
+__global__ __launch_bounds__(256) void decode_join_kernel(CacheGeom g, const int32_t *__restrict__ lengths,
+                                                          const float *__restrict__ parts, uint16_t *__restrict__ O,
+                                                          float *__restrict__ lse)
+{
+    constexpr int N = D / 64;
+    const int lane = threadIdx.x & 63;
+    const int row = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    if (row >= g.B * g.Hq) return;
+    const int s = row / g.Hq, a = row - s * g.Hq;
+    const DecodePart p = decode_plan(g, lengths, -1, s);
+    if (p.parts <= 1) return;
+    const int groups = (g.G + 15) / 16, heads = g.Hkv * groups;
+    const int kv = a / g.G, hh = kv * groups + (a - kv * g.G) / 16, col = (a - kv * g.G) & 15;
+    const float *from = parts + ((size_t)p.item0 * heads + hh) * decode_part_floats(D);
+    const size_t step = (size_t)heads * decode_part_floats(D);
+    float M = -INFINITY, L = 0.f, o[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) o[k] = 0.f;
+    for (int i0 = 0; i0 < p.parts; i0 += 64) {  // 64 parts at a time: lane i has the weight of part i0 + i
+        const bool in = i0 + lane < p.parts;
+        const float *ml = from + (size_t)(i0 + (in ? lane : 0)) * step + 16 * D + col;
+        const float m = in ? ml[0] : -INFINITY, l = in ? ml[16] : 0.f;
+        float top = m;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+        const float M1 = fmaxf(M, top);
+        if (M1 == -INFINITY) continue;  // (no part so far has a key)
+        const float keep = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - M1), w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M1);
+        float lw = l * w;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) lw += __shfl_xor(lw, d, 64);
+        L = L * keep + lw;
+        M = M1;
+#pragma unroll
+        for (int k = 0; k < N; ++k) o[k] *= keep;
+        const int n = min(64, p.parts - i0);
+        for (int i = 0; i < n; i += 4) {  // four parts' loads at a time (past the last one it is read again, with a weight of 0)
+            float x[4][N];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int k = 0; k < N; ++k) x[u][k] = from[(size_t)(i0 + min(i + u, n - 1)) * step + col * D + N * lane + k];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float wi = i + u < n ? __shfl(w, i + u, 64) : 0.f;
+#pragma unroll
+                for (int k = 0; k < N; ++k) o[k] = fmaf(wi, x[u][k], o[k]);
+            }
+        }
+    }
+    const float inv = L > 0.f ? 1.0f / L : 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) reinterpret_cast<__bf16 *>(O)[(size_t)row * D + N * lane + k] = (__bf16)(o[k] * inv);
+    if (lse != nullptr && lane == 0) lse[row] = (M + log2f(L)) * 0.69314718055994530942f;
+}
+
+size_t decode_workspace_bytes(const CacheGeom &g)
+{
+    const int parts = decode_parts(g);
+    return parts > g.B ? (size_t)parts * g.Hkv * ((g.G + 15) / 16) * decode_part_floats(g.D) * 4 : 0;
+}
+
+template <int D, bool E4M3>
+static hipError_t launch_decode(const CacheGeom &g, const uint16_t *Q, const int32_t *table, const int32_t *lengths,
+                                const CacheData &c, uint16_t *O, float *lse, float *parts, hipStream_t st)
+{
+    using C = Decode<D, E4M3>;
+    static LdsOptIn opted;  // one per kernel instantiation
+    const hipError_t e = opted.ensure(reinterpret_cast<const void *>(&decode_attn_kernel<D, E4M3>), C::BYTES);
+    if (e != hipSuccess) return e;
+    const unsigned heads = (unsigned)(g.Hkv * ((g.G + 15) / 16));
+    hipLaunchKernelGGL((decode_attn_kernel<D, E4M3>), dim3((unsigned)decode_parts(g) * heads), dim3(C::THREADS), C::BYTES, st, g, Q,
+                       table, lengths, static_cast<const unsigned char *>(c.K), static_cast<const unsigned char *>(c.V), c.ks,
+                       c.vs, O, lse, parts);
+    if (decode_parts(g) > g.B)
+        hipLaunchKernelGGL((decode_join_kernel<D>), dim3((unsigned)((g.B * g.Hq + 3) / 4)), dim3(256), 0, st, g, lengths, parts, O, lse);
+    return hipGetLastError();
+}
+
+hipError_t launch_decode_attn(const CacheGeom &g, const uint16_t *Q, const int32_t *table, const int32_t *lengths,
+                              const CacheData &c, uint16_t *O, float *lse, void *ws, hipStream_t st)
+{
+    float *parts = static_cast<float *>(ws);
+    if (g.D == 64) return g.e4m3 ? launch_decode<64, true>(g, Q, table, lengths, c, O, lse, parts, st)
+                                 : launch_decode<64, false>(g, Q, table, lengths, c, O, lse, parts, st);
+    return g.e4m3 ? launch_decode<128, true>(g, Q, table, lengths, c, O, lse, parts, st)
+                  : launch_decode<128, false>(g, Q, table, lengths, c, O, lse, parts, st);
+}
+
+}  // namespace adaspark

@@ -1,0 +1,543 @@
+// Backward pass of attention over packed prompts (prompt.h).  For a row with keys A, c = 1/sqrt(D), p = softmax(c q.k),
+// delta = dO.O:
+//     dV_j += p_j dO,   dS_j = p_j (dO.v_j - delta),   dQ = c sum_j dS_j k_j,   dK_j += c dS_j q
+// with dK, dV summed over the G heads of a KV head's group.  p is rebuilt from the log-sum-exp.  As in the backward of the cube-selective
+// attention (attn_bwd.hip) two kernels, one that keeps rows and one that keeps keys, do it without atomics: seven products
+// where five would do with them, and the same bits every time.
+//   prompt_dq_kernel   256 rows of a (sequence, KV head), 32 to a wavefront with Q and dO in registers, over tiles of 64 keys:
+//                      S^T = K.Q^T, dP^T = V.dO^T, dQ^T += K^T.dS^T.
+//   prompt_dkv_kernel  256 keys, 32 to a wavefront with K and V in registers, over tiles of 64 rows:
+//                      S = Q.K^T, dP = dO.V^T, dV^T += dO^T.P, dK^T += Q^T.dS.
+// All tiles are rows as the caller holds them, read in LDS both ways (rowtile.h).  The accumulators of S start from
+// -lse * sqrt(D) and those of dP from -delta, which prompt_prep_kernel leaves per row.
+// Score products are exact; p and dS are rounded to bf16 as operands of the other products, sums are fp32.
+//
+// Where few key blocks have long walks, a walk is cut into spans of equal length, a workgroup each, which leave fp32 sums in the
+// workspace; prompt_reduce_kernel adds them in their order.
+#include <algorithm>
+
+#include "prompt.h"
+
+namespace adaspark {
+
+constexpr int PB_THREADS = 512;
+constexpr int PB_BLOCK = 256;  // rows (dQ) or keys (dK, dV) of a workgroup: 8 wavefronts x 2 x 16
+
+template <int D>
+struct PromptBwd {
+    static constexpr int TILE = 64 * D * 2;
+    static constexpr int CPR = D / 8, RPI = 64 / CPR;
+    static constexpr int PER = 64 / RPI / 8;  // direct-to-LDS instructions per wavefront, tile and operand
+    static constexpr int OFF_LSE = 2 * TILE;  // behind the two tiles (dK/dV kernel): 64 start values of S, 64 of dP
+    static constexpr int STAGE = 2 * TILE + 512;
+    static constexpr int NST = 3;
+    static constexpr int BYTES = NST * STAGE;
+    static_assert(BYTES <= 160 * 1024, "LDS of one CU");
+};
+
+// ---- the spans of the dK/dV kernel
+struct PromptSpans {
+    long long blocks;  // bound of the key blocks per KV head
+    int tiles;         // row tiles of a span
+    int most;          // spans of a block at most
+};
+static long long key_block_bound(const PromptGeom &g) { return (long long)g.Tk / PB_BLOCK + g.B; }
+__device__ __forceinline__ int key_block_id(int s, int k0, int j) { return k0 / PB_BLOCK + s + j; }
+
+// What is known here are the tokens of all sequences, so the cut is that of one sequence of them all: spans of a length
+// that gives about three workgroups per CU, eight tiles at least (a span's sums are written and read again, about as much time as two tiles
+// take); shorter sequences then have fewer spans, or one, which writes its gradients itself.
+static PromptSpans prompt_spans(const PromptGeom &g)
+{
+    PromptSpans s;
+    s.blocks = key_block_bound(g);
+    const long long tiles = ((long long)g.Tq * g.G + 63) / 64;
+    const long long total = s.blocks * g.Hkv * tiles / (g.causal ? 2 : 1);
+    s.tiles = (int)std::max(8ll, std::min((total + 767) / 768, std::max(1ll, tiles)));
+    s.most = (int)std::max(1ll, (tiles + s.tiles - 1) / s.tiles);
+    if (s.most == 1) s.tiles = (int)std::max(1ll, tiles);
+    return s;
+}
+
+struct PromptBwdWorkspace {
+    float *lse2, *delta;  // [Tq * Hq + 1]: entry [Tq * Hq] belongs to the rows that pad a tile: -inf, 0
+    float *part;          // [Hkv][blocks][most][2 (dV, dK)][256 x D] in MFMA output order
+    size_t bytes;
+};
+static PromptBwdWorkspace bwd_workspace_of(const PromptGeom &g, int D, void *ws)
+{
+    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    const PromptSpans s = prompt_spans(g);
+    const size_t rows = up(((size_t)g.Tq * g.Hq + 1) * 4);
+    unsigned char *p = static_cast<unsigned char *>(ws);
+    PromptBwdWorkspace w;
+    w.lse2 = reinterpret_cast<float *>(p);
+    w.delta = reinterpret_cast<float *>(p + rows);
+    w.part = reinterpret_cast<float *>(p + 2 * rows);
+    w.bytes = 2 * rows + (s.most > 1 ? (size_t)g.Hkv * s.blocks * s.most * 2 * PB_BLOCK * D * 4 : 0);
+    return w;
+}
+size_t prompt_bwd_workspace_bytes(const PromptGeom &g, int D) { return bwd_workspace_of(g, D, nullptr).bytes; }
+
+// Start values of every row: 256 / (D / 8) rows to a workgroup, D / 8 lanes to a row.  A row without keys (log-sum-exp -inf) gets
+// no part in anything.
+template <int D>
+__global__ __launch_bounds__(256) void prompt_prep_kernel(long long rows, const uint16_t *__restrict__ O, const uint16_t *__restrict__ dO,
+                                                          const float *__restrict__ lse, float *__restrict__ lse2,
+                                                          float *__restrict__ delta)
+{
+    constexpr int CPR = D / 8;
+    const long long r = ((long long)blockIdx.x * 256 + threadIdx.x) / CPR;
+    const int col = threadIdx.x % CPR;
+    float part = 0.f;
+    if (r < rows) {
+        const bf16x8 a = *reinterpret_cast<const bf16x8 *>(dO + r * D + col * 8), b = *reinterpret_cast<const bf16x8 *>(O + r * D + col * 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) part = fmaf((float)a[e], (float)b[e], part);
+    }
+#pragma unroll
+    for (int d = CPR / 2; d >= 1; d >>= 1) part += __shfl_xor(part, d, 64);
+    if (col == 0 && r <= rows) {
+        const float l = r < rows ? lse[r] : -INFINITY;
+        lse2[r] = l == -INFINITY ? -INFINITY : -l * sqrtf((float)D);  // = -(lse in base 2) / (softmax scale in base 2)
+        delta[r] = -part;
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(PB_THREADS) void prompt_dq_kernel(PromptGeom g, int per_head, const uint16_t *__restrict__ Q,
+                                                               const uint16_t *__restrict__ K, const uint16_t *__restrict__ V,
+                                                               const uint16_t *__restrict__ dO, const float *__restrict__ lse2p,
+                                                               const float *__restrict__ deltap, uint16_t *__restrict__ dQ)
+{
+    using C = PromptBwd<D>;
+    constexpr int NS = 2, KSTEPS = D / 32, DT = D / 16;
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    const int lane = threadIdx.x & 63, n16 = lane & 15, q4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    int kv, slot, seq, blk;
+    if (!head_slot(blockIdx.x, g.Hkv, per_head, kv, slot)) return;
+    if (!prompt_block(g, slot, (g.Tk + KEY_TILE - 1) / KEY_TILE,
+                      [&](int n, int m, int t) { return row_blocks<PB_BLOCK>(n, m, g.G, g.causal, t); }, seq, blk))
+        return;
+    seq = __builtin_amdgcn_readfirstlane(seq);
+    const PromptSeq p = prompt_seq(g, seq);
+    const int rows = p.n * g.G, row0 = ((rows - 1) / PB_BLOCK - blk) * PB_BLOCK;
+    auto reach_of = [&](int row) { return g.causal ? p.m - p.n + token_of_row(g, row) : p.m - 1; };
+    auto tiles_to = [&](int row) {
+        const int r = reach_of(min(row, rows - 1));
+        return r < 0 ? 0 : r / KEY_TILE + 1;
+    };
+    const int ntiles = __builtin_amdgcn_readfirstlane(tiles_to(row0 + PB_BLOCK - 1));
+    const int mine = row0 + 32 * wave < rows ? __builtin_amdgcn_readfirstlane(tiles_to(row0 + 32 * wave + 31)) : 0;
+
+    int reach[NS];
+    bool valid[NS];
+    size_t rid[NS];
+    float lse2[NS], delta[NS];
+    bf16x8 qf[NS][KSTEPS], gf[NS][KSTEPS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int row = row0 + 32 * wave + 16 * s + n16, r = min(row, rows - 1), tok = token_of_row(g, r);
+        valid[s] = row < rows;
+        reach[s] = reach_of(r);
+        const int head = kv * g.G + (r - tok * g.G);
+        rid[s] = (size_t)(p.q0 + tok) * g.Hq + head;
+        const uint16_t *q = Q + (size_t)(p.q0 + tok) * g.qs + (size_t)head * D + 8 * q4;
+#pragma unroll
+        for (int c = 0; c < KSTEPS; ++c) {
+            qf[s][c] = *reinterpret_cast<const bf16x8 *>(q + 32 * c);
+            gf[s][c] = *reinterpret_cast<const bf16x8 *>(dO + rid[s] * D + 8 * q4 + 32 * c);
+        }
+        lse2[s] = lse2p[rid[s]];
+        delta[s] = deltap[rid[s]];
+    }
+    const int reach_lo = __builtin_amdgcn_readfirstlane(reach[0]);
+
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem);
+    const uint16_t *khead = K + (size_t)p.k0 * g.ks + (size_t)kv * D, *vhead = V + (size_t)p.k0 * g.vs + (size_t)kv * D;
+    // (keys past the sequence's last are that one again)
+    auto issue = [&](int t, int stage) __attribute__((always_inline)) {
+        const int key = t * KEY_TILE, last = min(KEY_TILE - 1, p.m - 1 - key);
+        const void *kt = uniform_ptr(khead + (size_t)key * g.ks), *vt = uniform_ptr(vhead + (size_t)key * g.vs);
+#pragma unroll
+        for (int u = 0; u < C::PER; ++u) {
+            const int r = (wave * C::PER + u) * C::RPI + lane / C::CPR, chunk = (((lane & 15) ^ row_swizzle<D>(r)) & (C::CPR - 1)) * 8;
+            const uint32_t piece = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)(stage * C::STAGE + (wave * C::PER + u) * 1024));
+            dma_1k_s(piece, kt, (uint32_t)(min(r, last) * (int)g.ks + chunk) * 2u);
+            dma_1k_s(piece + C::TILE, vt, (uint32_t)(min(r, last) * (int)g.vs + chunk) * 2u);
+        }
+    };
+
+    f32x4 acc[NS][DT];
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int e = 0; e < DT; ++e) acc[s][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float c2 = 1.44269504088896340736f / sqrtf((float)D);  // softmax scale in base 2
+    const uint32_t nat0 = (uint32_t)row_tile_off<D>(n16, q4);
+    const uint32_t tr0 = (uint32_t)(row_tile_off<D>(4 * q4 + (n16 >> 2), (n16 & 3) >> 1) + 8 * (n16 & 1));
+    constexpr int BLK = 16 * D * 2;
+
+    // One tile, in two halves of 32 keys (k index 8 q4 + 4 x + v of the last product: key 32 H + 16 x + 4 q4 + v).  The order
+    // written here is the order executed, operands one step ahead of their MFMAs.
+    auto work = [&](int t, int stage) __attribute__((always_inline)) {
+        const uint32_t nat = lds0 + (uint32_t)(stage * C::STAGE) + nat0, tr = lds0 + (uint32_t)(stage * C::STAGE) + tr0;
+        auto rows_at = [&](int blk, int c, bf16x8 (&o)[2]) __attribute__((always_inline)) {  // K, V
+            const uint32_t at = (nat ^ (uint32_t)(c << 6)) + (uint32_t)(blk * BLK);
+            o[0] = lds_read<bf16x8>(at);
+            o[1] = lds_read<bf16x8>(at + C::TILE);
+        };
+        auto cols_at = [&](int H, int e) __attribute__((always_inline)) {  // K^T
+            return lds_read_tr2((tr ^ (uint32_t)(e << 5)) + (uint32_t)(2 * H * BLK), BLK);
+        };
+        const bool edge = t * KEY_TILE + KEY_TILE - 1 > reach_lo;
+        bf16x8 op[2][2], tp[2];
+        rows_at(0, 0, op[0]);
+#pragma unroll
+        for (int H = 0; H < 2; ++H) {
+            bf16x8 ds[NS];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                f32x4 sa[NS], pa[NS];
+#pragma unroll
+                for (int k = 0; k < KSTEPS; ++k) {
+                    if (k + 1 < KSTEPS) rows_at(2 * H + x, k + 1, op[(k + 1) & 1]);
+                    else if (x == 0) rows_at(2 * H + 1, 0, op[(k + 1) & 1]);
+                    else tp[0] = cols_at(H, 0);
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        sa[s] = mfma16(op[k & 1][0], qf[s][k], k == 0 ? f32x4{lse2[s], lse2[s], lse2[s], lse2[s]} : sa[s]);
+                        pa[s] = mfma16(op[k & 1][1], gf[s][k], k == 0 ? f32x4{delta[s], delta[s], delta[s], delta[s]} : pa[s]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (edge) {
+                    const int key = t * KEY_TILE + 32 * H + 16 * x + 4 * q4;
+#pragma unroll
+                    for (int s = 0; s < NS; ++s)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            if (key + v > reach[s]) sa[s][v] = -INFINITY;
+                }
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        ds[s][4 * x + v] = (__bf16)(__builtin_amdgcn_exp2f(sa[s][v] * c2) * pa[s][v]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int e = 0; e < DT; ++e) {
+                if (e + 1 < DT) tp[(e + 1) & 1] = cols_at(H, e + 1);
+                else if (H == 0) rows_at(2, 0, op[0]);
+#pragma unroll
+                for (int s = 0; s < NS; ++s) acc[s][e] = mfma16(tp[e & 1], ds[s], acc[s][e]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+    static_assert(KSTEPS % 2 == 0 && DT % 2 == 0, "the operands' two places take turns");
+
+    if (ntiles > 0) issue(0, 0);
+    if (ntiles > 1) issue(1, 1);
+    for (int t = 0, stage = 0; t < ntiles; ++t, stage = stage == 2 ? 0 : stage + 1) {
+        if (t + 1 < ntiles) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * C::PER) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t + 2 < ntiles) issue(t + 2, stage == 0 ? 2 : stage - 1);  // (the stage read last at tile t - 1)
+        if (t < mine) work(t, stage);
+    }
+    const float c = 1.0f / sqrtf((float)D);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        if (!valid[s]) continue;
+        uint16_t *o = dQ + rid[s] * D + 4 * q4;
+#pragma unroll
+        for (int e = 0; e < DT; ++e) *reinterpret_cast<uint2 *>(o + 16 * e) = pack_bf16(acc[s][e] * c);
+    }
+}
+
+// Key blocks of a sequence whose walk over the rows has at least t tiles of 64; the first blocks walk farthest.
+__device__ __forceinline__ int key_blocks(int n, int m, int G, int causal, int t)
+{
+    const int nb = (m + PB_BLOCK - 1) / PB_BLOCK;
+    if (t == 0) return nb;
+    const long long rows = (long long)n * G - 64ll * (t - 1);  // a block has such a walk if its first row lies before this one
+    if (rows <= 0) return 0;
+    if (!causal) return nb;
+    const long long key = (rows - 1) / G + (m - n);  // the last key whose first row does
+    return key < 0 ? 0 : (int)min((long long)nb, key / PB_BLOCK + 1);
+}
+
+template <int D>
+__global__ __launch_bounds__(PB_THREADS) void prompt_dkv_kernel(PromptGeom g, int per_head, PromptSpans cut,
+                                                                const uint16_t *__restrict__ Q, const uint16_t *__restrict__ K,
+                                                                const uint16_t *__restrict__ V, const uint16_t *__restrict__ dO,
+                                                                const float *__restrict__ lse2p, const float *__restrict__ deltap,
+                                                                float *__restrict__ partial, uint16_t *__restrict__ dK,
+                                                                uint16_t *__restrict__ dV)
+{
+    using C = PromptBwd<D>;
+    constexpr int NS = 2, KSTEPS = D / 32, DT = D / 16, PER = C::PER;
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    const int lane = threadIdx.x & 63, n16 = lane & 15, q4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    int kv, slot, seq, j;
+    if (!head_slot(blockIdx.x, g.Hkv, per_head, kv, slot)) return;
+    const int span = slot % cut.most;
+    if (!prompt_block(g, slot / cut.most, (int)(((long long)g.Tq * g.G + 63) / 64),
+                      [&](int n, int m, int t) { return key_blocks(n, m, g.G, g.causal, t); }, seq, j))
+        return;
+    seq = __builtin_amdgcn_readfirstlane(seq);
+    j = __builtin_amdgcn_readfirstlane(j);
+    const PromptSeq p = prompt_seq(g, seq);
+    const int rows = p.n * g.G, off = p.m - p.n;
+    auto first_row = [&](int key) { return g.causal ? (int)min((long long)rows, max(0ll, (long long)key - off) * g.G) : 0; };  // that attends it
+    const int first = first_row(j * PB_BLOCK);
+    const int all = (rows - first + 63) / 64, spans = max(1, (all + cut.tiles - 1) / cut.tiles);
+    if (span >= spans) return;
+    const int row0 = first + span * cut.tiles * 64, ntiles = min(cut.tiles, all - span * cut.tiles);
+
+    const int key0 = j * PB_BLOCK + wave * 32;
+    const bool busy = key0 < p.m;
+    const int mine_from = first_row(key0);                       // no row before it attends a key of the wavefront
+    const int mine_all = first_row(min(key0 + 31, p.m - 1));     // from it on all rows attend all of them
+
+    bf16x8 kf[NS][KSTEPS], vf[NS][KSTEPS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int key = min(key0 + 16 * s + n16, p.m - 1);
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k) {
+            kf[s][k] = *reinterpret_cast<const bf16x8 *>(K + (size_t)(p.k0 + key) * g.ks + (size_t)kv * D + 32 * k + 8 * q4);
+            vf[s][k] = *reinterpret_cast<const bf16x8 *>(V + (size_t)(p.k0 + key) * g.vs + (size_t)kv * D + 32 * k + 8 * q4);
+        }
+    }
+    f32x4 accV[NS][DT], accK[NS][DT];
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int e = 0; e < DT; ++e) accV[s][e] = accK[s][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    const float c2 = 1.44269504088896340736f / sqrtf((float)D);  // softmax scale in base 2
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem);
+    auto fresh_lane = [&]() __attribute__((always_inline)) {  // registers are short: what depends on the lane is worked out anew for every tile
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
+    // Tile t of the span.  Rows past the sequence's last are that one again, under start values that give them no part.
+    auto issue = [&](int t, int stage) __attribute__((always_inline)) {
+        const uint32_t dst = lds0 + (uint32_t)(stage * C::STAGE);
+        const int l = fresh_lane(), r0 = row0 + 64 * t;
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const int r = (wave * PER + u) * C::RPI + l / C::CPR;
+            const int row = min(r0 + r, rows - 1), tok = token_of_row(g, row), head = kv * g.G + (row - tok * g.G);
+            const int chunk = (((l & 15) ^ row_swizzle<D>(r)) & (C::CPR - 1)) * 8;
+            const uint32_t piece = __builtin_amdgcn_readfirstlane(dst + (uint32_t)((wave * PER + u) * 1024));
+            dma_lane16(piece, Q + (size_t)(p.q0 + tok) * g.qs + head * D + chunk);
+            dma_lane16(piece + C::TILE, dO + ((size_t)(p.q0 + tok) * g.Hq + head) * D + chunk);
+        }
+        if (wave < 2) {  // the start values: wavefront 0 of S, wavefront 1 of dP
+            const int row = r0 + l, tok = token_of_row(g, row);
+            const size_t at = row < rows ? (size_t)(p.q0 + tok) * g.Hq + kv * g.G + (row - tok * g.G) : (size_t)g.Tq * g.Hq;
+            dma_lane4(__builtin_amdgcn_readfirstlane(dst + C::OFF_LSE + 256 * wave), (wave == 0 ? lse2p : deltap) + at);
+        }
+    };
+    const uint32_t nat0 = (uint32_t)row_tile_off<D>(n16, q4);
+    const uint32_t tr0 = (uint32_t)(row_tile_off<D>(4 * q4 + (n16 >> 2), (n16 & 3) >> 1) + 8 * (n16 & 1));
+    constexpr int BLK = 16 * D * 2;  // bytes of 16 tile rows
+
+    // One tile, in two halves of 32 rows.  EDGE: some row does not attend some key of the wavefront.  The order written here is
+    // the order executed (operands one step ahead of their MFMAs): left to itself the compiler starts more loads than there
+    // are registers for.
+    auto work = [&](int stage, int r0, auto edge_tag) __attribute__((always_inline)) {
+        constexpr bool EDGE = decltype(edge_tag)::value;
+        const uint32_t st = lds0 + (uint32_t)(stage * C::STAGE), nat = st + nat0, tr = st + tr0;
+        auto rows_at = [&](int blk, int k, bf16x8 (&o)[2]) __attribute__((always_inline)) {  // Q, dO
+            uint32_t at;
+            asm volatile("v_xor_b32 %0, %1, %2" : "=v"(at) : "n"(k << 6), "v"(nat));
+            o[0] = lds_read<bf16x8>(at + (uint32_t)(blk * BLK));
+            o[1] = lds_read<bf16x8>(at + (uint32_t)(blk * BLK + C::TILE));
+        };
+        auto cols_at = [&](int H, int e, bf16x8 (&o)[2]) __attribute__((always_inline)) {  // Q^T, dO^T
+            uint32_t at;
+            asm volatile("v_xor_b32 %0, %1, %2" : "=v"(at) : "n"(e << 5), "v"(tr));
+            o[0] = lds_read_tr2(at + (uint32_t)(2 * H * BLK), BLK);
+            o[1] = lds_read_tr2(at + (uint32_t)(2 * H * BLK + C::TILE), BLK);
+        };
+        bf16x8 op[2][2];
+        rows_at(0, 0, op[0]);
+#pragma unroll
+        for (int H = 0; H < 2; ++H) {
+            bf16x8 pp[NS], ds[NS];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {  // 16 rows: scores and dP
+                const uint32_t vec = st + (uint32_t)(C::OFF_LSE + 16 * (2 * H + x) * 4) + (uint32_t)(16 * q4);
+                const f32x4 li = lds_read<f32x4>(vec), di = lds_read<f32x4>(vec + 256);
+                f32x4 sa[NS], pa[NS];
+#pragma unroll
+                for (int k = 0; k < KSTEPS; ++k) {
+                    if (k + 1 < KSTEPS) rows_at(2 * H + x, k + 1, op[(k + 1) & 1]);
+                    else if (x == 0) rows_at(2 * H + 1, 0, op[(k + 1) & 1]);
+                    else cols_at(H, 0, op[(k + 1) & 1]);
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        sa[s] = mfma16(op[k & 1][0], kf[s][k], k == 0 ? li : sa[s]);
+                        pa[s] = mfma16(op[k & 1][1], vf[s][k], k == 0 ? di : pa[s]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (EDGE) {
+                    const int row = r0 + 16 * (2 * H + x) + 4 * q4;
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        const int from = first_row(key0 + 16 * s + n16);
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            if (row + v < from) sa[s][v] = -INFINITY;
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const float w = __builtin_amdgcn_exp2f(sa[s][v] * c2);
+                        pp[s][4 * x + v] = (__bf16)w;
+                        ds[s][4 * x + v] = (__bf16)(w * pa[s][v]);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // dV^T += dO^T.P, dK^T += Q^T.dS over the half's 32 rows (k index 8 q4 + 4 x + v: row 16 x + 4 q4 + v)
+#pragma unroll
+            for (int e = 0; e < DT; ++e) {
+                if (e + 1 < DT) cols_at(H, e + 1, op[(e + 1) & 1]);
+                else if (H == 0) rows_at(2, 0, op[(e + 1) & 1]);
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    accK[s][e] = mfma16(op[e & 1][0], ds[s], accK[s][e]);
+                    accV[s][e] = mfma16(op[e & 1][1], pp[s], accV[s][e]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+
+    if (ntiles > 0) issue(0, 0);
+    if (ntiles > 1) issue(1, 1);
+    int t = 0, stage = 0;
+    auto tile = [&](auto edge_tag) __attribute__((always_inline)) {
+        // this wavefront's loads of the tile have landed (those of the next may stay in flight), then everybody's
+        if (t + 1 >= ntiles) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else if (wave < 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * PER + 1) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * PER) : "memory");
+        if (t + 2 < ntiles) issue(t + 2, stage == 0 ? 2 : stage - 1);  // (the stage read last at tile t - 1)
+        const int r0 = row0 + 64 * t;
+        if (busy && (!decltype(edge_tag)::value || r0 + 63 >= mine_from)) work(stage, r0, edge_tag);
+        ++t;
+        stage = stage == 2 ? 0 : stage + 1;
+    };
+    while (t < ntiles && row0 + 64 * t < mine_all) tile(std::true_type{});
+    while (t < ntiles) tile(std::false_type{});
+
+    if (spans > 1) {
+        f32x4 *sums = reinterpret_cast<f32x4 *>(partial) +
+                      (((size_t)kv * cut.blocks + key_block_id(seq, p.k0, j)) * cut.most + span) * (2 * PB_BLOCK * D / 4) + wave * (NS * DT * 64) + lane;
+#pragma unroll
+        for (int x = 0; x < NS * DT; ++x) {
+            sums[x * 64] = accV[x / DT][x % DT];
+            sums[x * 64 + PB_BLOCK * D / 4] = accK[x / DT][x % DT];
+        }
+        return;
+    }
+    const float c = 1.0f / sqrtf((float)D);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int key = key0 + 16 * s + n16;
+        if (key >= p.m) continue;
+        const size_t o = ((size_t)(p.k0 + key) * g.Hkv + kv) * D + 4 * q4;
+#pragma unroll
+        for (int e = 0; e < DT; ++e) {
+            *reinterpret_cast<uint2 *>(dV + o + 16 * e) = pack_bf16(accV[s][e]);
+            *reinterpret_cast<uint2 *>(dK + o + 16 * e) = pack_bf16(accK[s][e] * c);
+        }
+    }
+}
+
+// The spans' sums of a key block, added in their order: eight workgroups to a block, one for each wavefront's keys; NS * DT * 64
+// places in MFMA output order.
+template <int D>
+__global__ __launch_bounds__(256) void prompt_reduce_kernel(PromptGeom g, PromptSpans cut, const float *__restrict__ partial,
+                                                            uint16_t *__restrict__ dK, uint16_t *__restrict__ dV)
+{
+    constexpr int NS = 2, DT = D / 16;
+    const int wave = blockIdx.x & 7, kv = (int)((blockIdx.x >> 3) % (unsigned)g.Hkv), id = (int)((blockIdx.x >> 3) / (unsigned)g.Hkv);
+    int lo = 0, hi = g.B;  // the sequence of block `id`: the last one whose blocks begin at or before it
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (key_block_id(mid, prompt_seq(g, mid).k0, 0) <= id) lo = mid;
+        else hi = mid;
+    }
+    const PromptSeq p = prompt_seq(g, lo);
+    const int j = id - key_block_id(lo, p.k0, 0);
+    if (j < 0 || j * (long long)PB_BLOCK >= p.m) return;
+    const long long rows = (long long)p.n * g.G, first = g.causal ? min(rows, max(0ll, (long long)j * PB_BLOCK - (p.m - p.n)) * g.G) : 0;
+    const int all = (int)((rows - first + 63) / 64), spans = (all + cut.tiles - 1) / cut.tiles;
+    if (spans <= 1) return;
+    const f32x4 *from = reinterpret_cast<const f32x4 *>(partial) + ((size_t)kv * cut.blocks + id) * cut.most * (2 * PB_BLOCK * D / 4) + wave * (NS * DT * 64);
+    const float c = 1.0f / sqrtf((float)D);
+    for (int x = threadIdx.x; x < NS * DT * 64; x += 256) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f}, k = v;
+#pragma unroll 2
+        for (int i = 0; i < spans; ++i) {
+            v += from[(size_t)i * (2 * PB_BLOCK * D / 4) + x];
+            k += from[(size_t)i * (2 * PB_BLOCK * D / 4) + PB_BLOCK * D / 4 + x];
+        }
+        const int lane = x & 63, e = (x >> 6) % DT, s = (x >> 6) / DT, key = j * PB_BLOCK + 32 * wave + 16 * s + (lane & 15);
+        if (key >= p.m) continue;
+        const size_t o = ((size_t)(p.k0 + key) * g.Hkv + kv) * D + 16 * e + 4 * (lane >> 4);
+        *reinterpret_cast<uint2 *>(dV + o) = pack_bf16(v);
+        *reinterpret_cast<uint2 *>(dK + o) = pack_bf16(k * c);
+    }
+}
+
+template <int D>
+static hipError_t launch_bwd(const PromptGeom &g, const uint16_t *Q, const uint16_t *K, const uint16_t *V, const uint16_t *O,
+                             const float *lse, const uint16_t *dO, uint16_t *dQ, uint16_t *dK, uint16_t *dV, void *ws, hipStream_t st)
+{
+    using C = PromptBwd<D>;
+    const PromptBwdWorkspace w = bwd_workspace_of(g, D, ws);
+    const PromptSpans cut = prompt_spans(g);
+    static LdsOptIn opted_q, opted_kv;
+    hipError_t e = opted_q.ensure(reinterpret_cast<const void *>(&prompt_dq_kernel<D>), C::BYTES);
+    if (e == hipSuccess) e = opted_kv.ensure(reinterpret_cast<const void *>(&prompt_dkv_kernel<D>), C::BYTES);
+    if (e != hipSuccess) return e;
+    const long long rows = (long long)g.Tq * g.Hq, per = 256 / (D / 8);
+    hipLaunchKernelGGL((prompt_prep_kernel<D>), dim3((unsigned)((rows + 1 + per - 1) / per)), dim3(256), 0, st, rows, O, dO, lse, w.lse2,
+                       w.delta);
+    if (g.Tk > 0) {
+        const int keys = (int)cut.blocks * cut.most;
+        hipLaunchKernelGGL((prompt_dkv_kernel<D>), dim3(head_grid(g.Hkv, keys)), dim3(PB_THREADS), C::BYTES, st, g, keys, cut, Q, K, V, dO,
+                           w.lse2, w.delta, w.part, dK, dV);
+        if (cut.most > 1)
+            hipLaunchKernelGGL((prompt_reduce_kernel<D>), dim3((unsigned)(cut.blocks * g.Hkv * 8)), dim3(256), 0, st, g, cut, w.part, dK, dV);
+    }
+    if (g.Tq > 0) {
+        const int blocks = (int)row_block_bound(g, PB_BLOCK);
+        hipLaunchKernelGGL((prompt_dq_kernel<D>), dim3(head_grid(g.Hkv, blocks)), dim3(PB_THREADS), C::BYTES, st, g, blocks, Q, K, V, dO,
+                           w.lse2, w.delta, dQ);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_prompt_bwd(const PromptGeom &g, int D, const uint16_t *Q, const uint16_t *K, const uint16_t *V, const uint16_t *O,
+                             const float *lse, const uint16_t *dO, uint16_t *dQ, uint16_t *dK, uint16_t *dV, void *ws, hipStream_t st)
+{
+    return D == 64 ? launch_bwd<64>(g, Q, K, V, O, lse, dO, dQ, dK, dV, ws, st)
+                   : launch_bwd<128>(g, Q, K, V, O, lse, dO, dQ, dK, dV, ws, st);
+}
+
+}  // namespace adaspark

@@ -1,0 +1,301 @@
+"""The paged cache and the attention of single new tokens over it, on the GPU, against 64-bit references."""
+import math
+
+import pytest
+import torch
+
+import prompt_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2604_08077_amd import binding
+
+    binding.load()
+    return binding
+
+
+def make(B, heads, lengths, page, fmt, seed, spare=2, table_extra=1, dirt=None):
+    """A cache with scattered pages for `lengths`; `dirt`: what every byte of it holds before (default zero)."""
+    need = [(m + page - 1) // page for m in lengths]
+    pages, table_pages = sum(need) + spare, max(need) + table_extra
+    sh = B.CacheShape(len(lengths), pages, page, table_pages, *heads, fmt)
+    cache = B.alloc_cache(sh)
+    if dirt is not None:
+        for t in cache:
+            if t is not None:
+                t.view(torch.uint8).fill_(dirt)
+    order = torch.randperm(pages, generator=torch.Generator().manual_seed(seed))
+    table, at = torch.full((len(lengths), table_pages), -1, dtype=torch.int32), 0
+    for s, n in enumerate(need):
+        table[s, :n] = order[at:at + n]
+        at += n
+    return sh, cache, table.cuda(), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+
+
+def tokens(heads, n, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return [torch.randn((n, heads[1], heads[2]), generator=g, device="cuda").bfloat16() for _ in range(2)]
+
+
+def held(cache_t, scale, table, s, m, page):
+    """Positions 0 .. m of sequence s in 64 bits, [m, Hkv, D]; NaN where a scale is."""
+    n = (m + page - 1) // page
+    x = cache_t[table[s, :n].long()].double()
+    if scale is not None:
+        x = x * scale[table[s, :n].long()].double()[..., None]
+    return x.permute(0, 2, 1, 3).reshape(-1, x.shape[1], x.shape[3])[:m]
+
+
+HEADS = [(4, 4, 64), (6, 2, 128), (28, 4, 128), (7, 1, 64)]
+
+
+@pytest.mark.parametrize("heads", HEADS[:3])
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("page", [1, 16, 128])
+def test_write_then_read(B, heads, fmt, page):
+    lengths, new = [130, 1, 0, 77, 300], [130, 1, 0, 5, 40]
+    sh, cache, table, dev_len = make(B, heads, lengths, page, fmt, 1)
+    before = [None if t is None else t.view(torch.uint8).clone() for t in cache]
+    K, V = tokens(heads, sum(new), 3)
+    K[2, 0] = 0  # a row of zeros
+    K[3] *= 2.0 ** -20
+    V[4] *= 2.0 ** 30
+    start = R.starts(new).cuda()
+    B.cache_write(sh, K, V, start, cache, table, dev_len)
+    first = [m - n for m, n in zip(lengths, new)]
+    Kr, Vr = B.cache_read(sh, cache, table, R.starts(lengths).cuda(), sum(lengths))
+    at = 0
+    for s, (m, n, f) in enumerate(zip(lengths, new, first)):
+        base = sum(lengths[:s])
+        for x, back, t, scale in ((K, Kr, cache.K, cache.k_scale), (V, Vr, cache.V, cache.v_scale)):
+            x, mine = x[at:at + n].double(), held(t, scale, table, s, m, page)
+            if n == 0:
+                continue
+            if fmt == "bf16":
+                assert torch.equal(mine[f:], x)
+            else:
+                amax = x.abs().amax(-1, keepdim=True)
+                sc = held(scale[..., None].contiguous(), None, table, s, m, page)[f:]
+                assert ((sc - amax / 448).abs() <= 2 * R.U32 * amax / 448).all()
+                # a code is the nearest to x / scale, whose fp32 value (a reciprocal and a product) is off by three roundings
+                y = torch.where(sc > 0, x / sc, torch.zeros_like(x))
+                step = torch.exp2(torch.floor(torch.log2(y.abs().clamp_min(2.0 ** -30))).clamp_min(-6) - 3)
+                code = torch.where(sc > 0, mine[f:] / sc, torch.zeros_like(x))
+                assert ((code - y).abs() <= step / 2 + 4 * R.U32 * y.abs()).all()
+            # read back: one rounding to bf16 (none in bf16)
+            got, want = back[base:base + m].double(), mine
+            assert ((got - want).abs() <= (R.U16 if fmt == "e4m3" else 0) * want.abs()).all()
+        at += n
+    # what was not written stays
+    written = torch.zeros((sh.pages, page), dtype=torch.bool, device="cuda")
+    for s, (m, f) in enumerate(zip(lengths, first)):
+        for pos in range(f, m):
+            written[int(table[s, pos // page]), pos % page] = True
+    for t, b in zip(cache, before):
+        if t is not None:
+            rest = ~written[:, None].expand(-1, heads[1], -1)
+            shape = (sh.pages, heads[1], page, -1)
+            assert torch.equal(t.view(torch.uint8).reshape(shape)[rest], b.reshape(shape)[rest])
+
+
+def test_rows_that_are_not_finite_and_tiny_rows(B):
+    heads, page = (2, 2, 64), 16
+    sh, cache, table, lengths = make(B, heads, [6], page, "e4m3", 1)
+    K, V = tokens(heads, 6, 1)
+    K[0, 0, 5], K[1, 1, 7], V[2, 0, 63] = math.inf, math.nan, -math.inf
+    K[3] = 2.0 ** -130  # below the smallest normal float: bf16 has it as a denormal
+    K[4] = 3.0e38
+    B.cache_write(sh, K, V, R.starts([6]).cuda(), cache, table, lengths)
+    Kr, Vr = B.cache_read(sh, cache, table, R.starts([6]).cuda(), 6)
+    assert Kr[0, 0].isnan().all() and Kr[1, 1].isnan().all() and Vr[2, 0].isnan().all()
+    assert Kr[0, 1].isfinite().all() and Kr[1, 0].isfinite().all() and Vr[2, 1].isfinite().all()
+    assert Kr[3].isfinite().all() and (Kr[3].abs() <= 2.0 ** -126).all()
+    assert ((Kr[4].double() - 3.0e38).abs() <= 2.0 ** -4 * 3.1e38).all()
+
+
+def test_tokens_without_a_place(B):
+    """Positions below 0, entries that are no page, positions beyond the table: not written, read as zero."""
+    heads, page = (4, 2, 64), 16
+    for fmt in ("bf16", "e4m3"):
+        sh, cache, table, _ = make(B, heads, [40, 40, 40], page, fmt, 1, table_extra=0)
+        table[0, 1], table[1, 0], table[1, 2] = -1, sh.pages, 2 ** 31 - 1
+        lengths = torch.tensor([40, 40, 60], dtype=torch.int32, device="cuda")  # the last: beyond its 48 positions
+        K, V = tokens(heads, 170, 2)
+        before = [t.clone().view(torch.uint8) for t in cache if t is not None]
+        B.cache_write(sh, K, V, torch.tensor([0, 40, 100, 170], dtype=torch.int32, device="cuda"), cache, table, lengths)
+        Kr, Vr = B.cache_read(sh, cache, table, R.starts([48, 48, 48]).cuda(), 144)
+        tol = 0 if fmt == "bf16" else 2.0 ** -3
+        near = lambda a, b: ((a.double() - b.double()).abs() <= tol * b.double().abs().amax(-1, keepdim=True)).all()  # noqa: E731
+        assert near(Kr[:16], K[:16]) and not Kr[16:32].any() and near(Kr[32:40], K[32:40])
+        # sequence 1: 60 tokens for 40 positions, the first 20 fall below 0; only page 1 is a page
+        assert not Kr[48:64].any() and near(Vr[64:80], V[40 + 20 + 16:40 + 20 + 32]) and not Vr[80:96].any()
+        # sequence 2: 70 tokens end at position 60: the first 10 fall below 0, those from 48 on have no page
+        assert near(Kr[96:144], K[100 + 10:100 + 58])
+        assert len(before)
+
+
+@pytest.mark.parametrize("heads", HEADS + [(40, 2, 128)])
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("page,lengths", [(16, [1]), (16, [0, 5, 0]), (1, [33, 64]), (64, [2049]), (256, [100, 1, 700, 257, 64, 65]),
+                                          (16, [9000, 3]), (32, [31, 32, 33] * 30)])
+def test_decode(B, heads, fmt, page, lengths):
+    sh, cache, table, dev_len = make(B, heads, lengths, page, fmt, 4, dirt=0xff)  # (every byte: NaN in either format, and scales of NaN)
+    total = sum(lengths)
+    K, V = tokens(heads, total, 6)
+    B.cache_write(sh, K, V, R.starts(lengths).cuda(), cache, table, dev_len)
+    Q = torch.randn((len(lengths), heads[0], heads[2]), generator=torch.Generator(device="cuda").manual_seed(8), device="cuda").bfloat16()
+    O, lse = B.decode_attn(sh, Q, cache, table, dev_len, return_lse=True)
+    check_decode(sh, Q, cache, table, lengths, page, O, lse)
+    assert torch.equal(O, B.decode_attn(sh, Q, cache, table, dev_len))
+
+
+def check_decode(sh, Q, cache, table, lengths, page, O, lse):
+    k = torch.cat([held(cache.K, cache.k_scale, table, s, m, page) for s, m in enumerate(lengths)])
+    v = torch.cat([held(cache.V, cache.v_scale, table, s, m, page) for s, m in enumerate(lengths)])
+    ref = R.attention(Q, k, v, [1] * len(lengths), lengths)
+    assert torch.isfinite(O).all()
+    # (in 8 bits the key's scale multiplies the score and the value's scale the weight, in fp32: two more roundings)
+    ref["off"] += 4 * R.U32 * (1 + ref["lse"].abs().nan_to_num(posinf=0.0))
+    worst = float(((O.double() - ref["O"]).abs() / R.output_bound(ref)).max())
+    assert worst <= 1, f"O: {worst:.2f} of its bound"
+    none = torch.isneginf(ref["lse"])
+    assert torch.equal(none, torch.isneginf(lse)) and not O[none].any()
+    d = torch.where(none, torch.zeros_like(ref["lse"]), lse.double() - ref["lse"]).abs()
+    worst = float((d / R.lse_bound(ref, max(lengths))).max())
+    assert worst <= 1, f"lse: {worst:.2f} of its bound"
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_decode_leaves_out_what_is_no_page(B, fmt):
+    heads, page, lengths = (8, 2, 128), 16, [300, 100]
+    sh, cache, table, dev_len = make(B, heads, lengths, page, fmt, 4, dirt=0xff)
+    K, V = tokens(heads, 400, 6)
+    B.cache_write(sh, K, V, R.starts(lengths).cuda(), cache, table, dev_len)
+    gone = table.clone()
+    gone[0, 3], gone[0, 18], gone[1, :] = -1, 10 ** 9, sh.pages
+    Q = torch.randn((2, 8, 128), generator=torch.Generator(device="cuda").manual_seed(8), device="cuda").bfloat16()
+    O, lse = B.decode_attn(sh, Q, cache, gone, torch.tensor([300, 10 ** 9], dtype=torch.int32, device="cuda"), return_lse=True)
+    keep = [p for p in range(300) if p // page not in (3, 18)]
+    k, v = (held(t, sc, table, 0, 300, page)[keep] for t, sc in ((cache.K, cache.k_scale), (cache.V, cache.v_scale)))
+    ref = R.attention(Q[:1], k, v, [1], [len(keep)])
+    ref["off"] += 4 * R.U32 * (1 + ref["lse"].abs())
+    assert float(((O[:1].double() - ref["O"]).abs() / R.output_bound(ref)).max()) <= 1
+    assert not O[1].any() and torch.isneginf(lse[1]).all()
+
+
+def test_decode_of_many_sequences_and_a_cache_beyond_32_bits(B):
+    heads, page = (4, 4, 128), 16
+    lengths = [1 + (i * 7) % 50 for i in range(700)]  # more than are shared out
+    sh, cache, table, dev_len = make(B, heads, lengths, page, "bf16", 4)
+    K, V = tokens(heads, sum(lengths), 6)
+    B.cache_write(sh, K, V, R.starts(lengths).cuda(), cache, table, dev_len)
+    Q = torch.randn((700, 4, 128), generator=torch.Generator(device="cuda").manual_seed(8), device="cuda").bfloat16()
+    O, lse = B.decode_attn(sh, Q, cache, table, dev_len, return_lse=True)
+    check_decode(sh, Q, cache, table, lengths, page, O, lse)
+    del cache
+    pages = (1 << 32) // (16 * 4 * 128 * 2) + 40  # the last pages lie beyond 2^32 bytes
+    sh = B.CacheShape(1, pages, page, 20, *heads, "bf16")
+    cache = B.alloc_cache(sh)
+    table = torch.arange(pages - 20, pages, dtype=torch.int32, device="cuda").view(1, 20)
+    K, V = tokens(heads, 300, 6)
+    one = torch.tensor([300], dtype=torch.int32, device="cuda")
+    B.cache_write(sh, K, V, R.starts([300]).cuda(), cache, table, one)
+    Kr, Vr = B.cache_read(sh, cache, table, R.starts([300]).cuda(), 300)
+    assert torch.equal(Kr, K) and torch.equal(Vr, V)
+    O, lse = B.decode_attn(sh, Q[:1], cache, table, one, return_lse=True)
+    check_decode(sh, Q[:1], cache, table, [300], page, O, lse)
+
+
+def test_a_conversation(B):
+    """As they are used together: a batch of prompts is prefilled and written to the cache, answers are decoded token by token, a
+    follow-up turn attends the history read back -- each step against the reference over all tokens so far."""
+    heads, page, prompts = (6, 2, 128), 16, [70, 33, 1]
+    Hq, Hkv, D = heads
+    sh = B.CacheShape(3, 40, page, 12, *heads, "bf16")
+    cache = B.alloc_cache(sh)
+    table = torch.randperm(36, generator=torch.Generator().manual_seed(1)).to(torch.int32).view(3, 12).cuda()
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rand = lambda n, h: torch.randn((n, h, D), generator=g, device="cuda").bfloat16()  # noqa: E731
+    hist = [[rand(0, Hkv), rand(0, Hkv)] for _ in prompts]
+
+    def grow(k, v, lens):
+        at = 0
+        for s, n in enumerate(lens):
+            hist[s] = [torch.cat([hist[s][0], k[at:at + n]]), torch.cat([hist[s][1], v[at:at + n]])]
+            at += n
+        return [len(h[0]) for h in hist]
+
+    def check(O, Q, lens):
+        k_len = [len(h[0]) for h in hist]
+        ref = R.attention(Q, torch.cat([h[0] for h in hist]), torch.cat([h[1] for h in hist]), lens, k_len)
+        assert float(((O.double() - ref["O"]).abs() / R.output_bound(ref)).max()) <= 1
+
+    lens = prompts
+    q, k, v = rand(sum(lens), Hq), rand(sum(lens), Hkv), rand(sum(lens), Hkv)
+    start = R.starts(lens).cuda()
+    total = torch.tensor(grow(k, v, lens), dtype=torch.int32, device="cuda")
+    O = B.prompt_attn(B.PromptShape(3, sum(lens), sum(lens), *heads), q, k, v, start)
+    B.cache_write(sh, k, v, start, cache, table, total)
+    check(O, q, lens)
+    for _ in range(5):
+        q, k, v = rand(3, Hq), rand(3, Hkv), rand(3, Hkv)
+        total = torch.tensor(grow(k, v, [1, 1, 1]), dtype=torch.int32, device="cuda")
+        B.cache_write(sh, k, v, R.starts([1, 1, 1]).cuda(), cache, table, total)
+        check(B.decode_attn(sh, q, cache, table, total), q, [1, 1, 1])
+    lens = [20, 0, 41]
+    q, k, v = rand(sum(lens), Hq), rand(sum(lens), Hkv), rand(sum(lens), Hkv)
+    k_len = grow(k, v, lens)
+    total = torch.tensor(k_len, dtype=torch.int32, device="cuda")
+    start, k_start = R.starts(lens).cuda(), R.starts(k_len).cuda()
+    B.cache_write(sh, k, v, start, cache, table, total)
+    Kr, Vr = B.cache_read(sh, cache, table, k_start, sum(k_len))
+    O = B.prompt_attn(B.PromptShape(3, sum(lens), sum(k_len), *heads), q, Kr, Vr, start, k_start)
+    check(O, q, lens)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_a_replayed_step(B, fmt):
+    """A decode step -- write the new token, attend -- captured once and replayed as the sequences grow."""
+    heads, page, lengths = (8, 2, 64), 16, [600, 37]
+    sh, cache, table, dev_len = make(B, heads, [m + 8 for m in lengths], page, fmt, 4)
+    K, V = tokens(heads, sum(lengths), 6)
+    base = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    B.cache_write(sh, K, V, R.starts(lengths).cuda(), cache, table, base)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    steps = [[torch.randn((2, h, 64), generator=g, device="cuda").bfloat16() for h in (8, 2, 2)] for _ in range(4)]
+    q, k, v = (t.clone() for t in steps[0])
+    one, ws = R.starts([1, 1]).cuda(), torch.empty(max(16, B.decode_workspace_bytes(sh)), dtype=torch.uint8, device="cuda")
+    O = torch.empty_like(q)
+    dev_len.copy_(base + 1)
+
+    def step():
+        B.cache_write(sh, k, v, one, cache, table, dev_len)
+        B.decode_attn(sh, q, cache, table, dev_len, O=O, workspace=ws)
+
+    eager = []
+    for i, s in enumerate(steps):
+        for dst, src in zip((q, k, v), s):
+            dst.copy_(src)
+        dev_len.copy_(base + 1 + i)
+        step()
+        torch.cuda.synchronize()
+        eager.append(O.clone())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(2):
+        for i, s in enumerate(steps):
+            for dst, src in zip((q, k, v), s):
+                dst.copy_(src)
+            dev_len.copy_(base + 1 + i)
+            O.fill_(1)
+            ws.fill_(255)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(O, eager[i])

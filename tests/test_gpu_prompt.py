@@ -1,0 +1,262 @@
+"""Attention over packed prompts and its backward on the GPU, against the formulas in 64 bits (prompt_reference.py), with
+tolerances per element derived from the kernels' roundings."""
+import math
+
+import pytest
+import torch
+
+import prompt_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2604_08077_amd import binding
+
+    binding.load()  # raises if the HIP library was not built: there is no fallback
+    return binding
+
+
+def inputs(heads, tq, tk, seed, scale=1.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    Hq, Hkv, D = heads
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    return [(rand(tq, Hq, D) * scale).bfloat16(), ((rand(tk, Hkv, D) + rand(1, Hkv, D)) * scale).bfloat16(), rand(tk, Hkv, D).bfloat16(),
+            rand(tq, Hq, D).bfloat16()]
+
+
+HEADS = [(4, 4, 64), (7, 1, 64), (6, 2, 128), (28, 4, 128)]
+LENGTHS = [
+    ([1], [1]),
+    ([0, 1, 0], [0, 1, 0]),
+    ([37, 1, 120, 5], None),
+    ([64, 256, 63], None),
+    ([5, 70, 0, 4], [3, 0, 9, 4]),        # rows before the first key, rows without any, keys without rows
+    ([130, 1, 3], [500, 257, 64]),        # follow-up turns
+    ([331, 700], None),
+    ([2], [1500]),
+    ([1025], None),
+]
+
+
+def check_forward(O, lse, ref, keys):
+    err = (O.double() - ref["O"]).abs()
+    assert torch.isfinite(O).all()
+    worst = float((err / R.output_bound(ref)).max())
+    assert worst <= 1, f"O: {worst:.2f} of its bound"
+    none = torch.isneginf(ref["lse"])
+    assert torch.equal(none, torch.isneginf(lse)) and not O[none].any()
+    d = torch.where(none, torch.zeros_like(ref["lse"]), lse.double() - ref["lse"]).abs()
+    worst = float((d / R.lse_bound(ref, keys)).max())
+    assert worst <= 1, f"lse: {worst:.2f} of its bound"
+
+
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("case", range(len(LENGTHS)))
+@pytest.mark.parametrize("causal", [True, False])
+def test_forward_and_gradients(B, heads, case, causal):
+    q_len, k_len = LENGTHS[case][0], LENGTHS[case][1] or LENGTHS[case][0]
+    tq, tk = sum(q_len), sum(k_len)
+    Q, K, V, dO = inputs(heads, tq, tk, 100 + case)
+    sh = B.PromptShape(len(q_len), tq, tk, *heads)
+    qs, ks = R.starts(q_len).cuda(), R.starts(k_len).cuda()
+    O, lse = B.prompt_attn(sh, Q, K, V, qs, ks, causal=causal, return_lse=True)
+    check_forward(O, lse, R.attention(Q, K, V, q_len, k_len, causal), max(k_len))
+    got = dict(zip(("dQ", "dK", "dV"), B.prompt_attn_bwd(sh, Q, K, V, O, lse, dO, qs, ks, causal=causal)))
+    want, tol = R.gradients(Q, K, V, O, lse, dO, q_len, k_len, causal)
+    for name, x in got.items():
+        worst = float(((x.double() - want[name]).abs() / tol[name]).max()) if x.numel() else 0.0
+        assert worst <= 1, f"{name}: {worst:.2f} of its bound"
+    again = B.prompt_attn_bwd(sh, Q, K, V, O, lse, dO, qs, ks, causal=causal)
+    assert all(torch.equal(a, b) for a, b in zip(got.values(), again)), "the same call, other bits"
+
+
+@pytest.mark.parametrize("heads,q_len,k_len,scale", [
+    ((40, 2, 128), [300, 9], None, 1.0),       # a group of twenty heads
+    ((12, 3, 128), [2100, 77], None, 1.0),     # three KV heads; spans of a walk
+    ((4, 4, 64), [4001], None, 1.0),
+    ((8, 8, 64), [3, 40], [9000, 5000], 1.0),  # keys shared out to many workgroups
+    ((6, 2, 128), [500], None, 4.0),           # scores in the hundreds
+    ((4, 2, 64), [1] * 600, [3] * 600, 1.0),   # more sequences than a wavefront holds at once
+])
+def test_long_and_large(B, heads, q_len, k_len, scale):
+    k_len = k_len or q_len
+    tq, tk = sum(q_len), sum(k_len)
+    Q, K, V, dO = inputs(heads, tq, tk, 7, scale)
+    sh = B.PromptShape(len(q_len), tq, tk, *heads)
+    qs, ks = R.starts(q_len).cuda(), R.starts(k_len).cuda()
+    O, lse = B.prompt_attn(sh, Q, K, V, qs, ks, return_lse=True)
+    check_forward(O, lse, R.attention(Q, K, V, q_len, k_len), max(k_len))
+    got = B.prompt_attn_bwd(sh, Q, K, V, O, lse, dO, qs, ks)
+    want, tol = R.gradients(Q, K, V, O, lse, dO, q_len, k_len)
+    for name, x in zip(("dQ", "dK", "dV"), got):
+        worst = float(((x.double() - want[name]).abs() / tol[name]).max())
+        assert worst <= 1, f"{name}: {worst:.2f} of its bound"
+
+
+def test_random_batches(B):
+    g = torch.Generator().manual_seed(11)
+    pick = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=g))  # noqa: E731
+    for trial in range(24):
+        heads = [(4, 4, 64), (8, 2, 64), (6, 2, 128), (14, 2, 128), (5, 5, 128)][pick(0, 4)]
+        q_len = [pick(0, 150) for _ in range(pick(1, 9))]
+        k_len = [max(0, n + pick(-20, 200)) for n in q_len]
+        causal = pick(0, 3) > 0
+        tq, tk = sum(q_len), sum(k_len)
+        Q, K, V, dO = inputs(heads, tq, tk, trial)
+        sh = B.PromptShape(len(q_len), tq, tk, *heads)
+        qs, ks = R.starts(q_len).cuda(), R.starts(k_len).cuda()
+        O, lse = B.prompt_attn(sh, Q, K, V, qs, ks, causal=causal, return_lse=True)
+        if tq:
+            check_forward(O, lse, R.attention(Q, K, V, q_len, k_len, causal), max(k_len))
+        got = B.prompt_attn_bwd(sh, Q, K, V, O, lse, dO, qs, ks, causal=causal)
+        want, tol = R.gradients(Q, K, V, O, lse, dO, q_len, k_len, causal)
+        for name, x in zip(("dQ", "dK", "dV"), got):
+            worst = float(((x.double() - want[name]).abs() / tol[name]).max()) if x.numel() else 0.0
+            assert worst <= 1, f"trial {trial} {heads} {q_len} {k_len} {causal} {name}: {worst:.2f} of its bound"
+
+
+def test_gradients_against_differences(B):
+    """The gradient of a loss sum(dO * O), O by the reference in 64 bits, against central differences of that loss."""
+    q_len, k_len, heads = [9, 2], [12, 2], (4, 2, 64)
+    Q, K, V, dO = inputs(heads, 11, 14, 5)
+    sh = B.PromptShape(2, 11, 14, *heads)
+    qs, ks = R.starts(q_len).cuda(), R.starts(k_len).cuda()
+    O, lse = B.prompt_attn(sh, Q, K, V, qs, ks, return_lse=True)
+    got = B.prompt_attn_bwd(sh, Q, K, V, O, lse, dO, qs, ks)
+    _, tol = R.gradients(Q, K, V, O, lse, dO, q_len, k_len)
+    ref = R.attention(Q, K, V, q_len, k_len)
+    base = [Q.double(), K.double(), V.double()]
+    loss = lambda x: (dO.double() * R.attention(*x, q_len, k_len)["O"]).sum()  # noqa: E731
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for i, (name, grad) in enumerate(zip(("dQ", "dK", "dV"), got)):
+        for _ in range(6):
+            d = torch.randn(base[i].shape, generator=g, device="cuda", dtype=torch.float64)
+            step = 1e-4
+            up, down = ([x + s * step * d if j == i else x for j, x in enumerate(base)] for s in (1, -1))
+            diff = float(loss(up) - loss(down)) / (2 * step)
+            # what each element may be off, and (dQ, dK) what delta is off through the rounding of O
+            bound = float((tol[name] * d.abs()).sum()) + 1e-6 * abs(diff) + 1e-6
+            if name != "dV":
+                e_delta = (dO.double().abs() * R.output_bound(ref)).sum(-1)  # [tokens, heads]
+                reach = float(K.double().abs().amax() if name == "dQ" else Q.double().abs().amax()) / math.sqrt(heads[2])
+                bound += float(e_delta.sum()) * reach * float(d.abs().amax()) * heads[2]
+            assert abs(float((grad.double() * d).sum()) - diff) <= bound, name
+
+
+def test_slices_of_a_fused_projection_and_rows_of_no_sequence(B):
+    heads, q_len = (6, 2, 128), [70, 300, 1]
+    Hq, Hkv, D = heads
+    T, gap = sum(q_len) + 12, 5
+    g = torch.Generator(device="cuda").manual_seed(2)
+    qkv = torch.randn((T, Hq + 2 * Hkv, D), generator=g, device="cuda").bfloat16()
+    qkv[:gap] = math.nan  # rows of no sequence may hold anything
+    qkv[gap + sum(q_len):] = math.inf
+    Q, K, V = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+    dO = torch.randn((T, Hq, D), generator=g, device="cuda").bfloat16()
+    starts = R.starts(q_len, gap).cuda()
+    sh = B.PromptShape(3, T, T, *heads)
+    O, lse = torch.full((T, Hq, D), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((T, Hq), 7.0, device="cuda")
+    B.prompt_attn(sh, Q, K, V, starts, O=O, lse=lse)
+    inside = slice(gap, gap + sum(q_len))
+    ref = R.attention(Q[inside], K[inside], V[inside], q_len, q_len)
+    check_forward(O[inside], lse[inside], ref, max(q_len))
+    dQ, dK, dV = (torch.full(t.shape, 7.0, dtype=torch.bfloat16, device="cuda") for t in (Q, K, V))
+    B.prompt_attn_bwd(sh, Q, K, V, O, lse, dO, starts, dQ=dQ, dK=dK, dV=dV)
+    want, tol = R.gradients(*(t[inside] for t in (Q, K, V, O, lse, dO)), q_len, q_len)
+    for name, x in (("dQ", dQ), ("dK", dK), ("dV", dV)):
+        assert float(((x[inside].double() - want[name]).abs() / tol[name]).max()) <= 1, name
+    for t in (O, lse, dQ, dK, dV):
+        outside = torch.cat([t[:gap], t[gap + sum(q_len):]])
+        assert (outside == 7).all(), "rows of no sequence were written"
+    # and the same as from contiguous tensors, bit for bit
+    assert torch.equal(O, B.prompt_attn(sh, Q.contiguous(), K.contiguous(), V.contiguous(), starts, O=O.clone()))
+
+
+def test_keys_behind_32_bit_offsets(B):
+    """A sequence whose keys lie beyond 2^32 bytes into K and V (and whose gradients do)."""
+    heads, n = (2, 2, 128), 200
+    T = (1 << 32) // (2 * 128 * 2) + 5000
+    K, V = (torch.zeros((T, 2, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q, k, v, dO = inputs(heads, n, n, 1)
+    K[T - n:], V[T - n:] = k, v
+    sh = B.PromptShape(1, n, T, *heads)
+    qs, ks = R.starts([n]).cuda(), torch.tensor([T - n, T], dtype=torch.int32, device="cuda")
+    O, lse = B.prompt_attn(sh, q, K, V, qs, ks, return_lse=True)
+    check_forward(O, lse, R.attention(q, k, v, [n], [n]), n)
+    dQ, dK, dV = B.prompt_attn_bwd(sh, q, K, V, O, lse, dO, qs, ks)
+    want, tol = R.gradients(q, k, v, O, lse, dO, [n], [n])
+    for name, x in (("dQ", dQ), ("dK", dK[T - n:]), ("dV", dV[T - n:])):
+        assert float(((x.double() - want[name]).abs() / tol[name]).max()) <= 1, name
+
+
+def test_starts_that_do_not_fit_stay_inside(B):
+    """Descending and far starts: nothing outside the tensors is touched (their neighbours in memory keep their values)."""
+    heads = (4, 2, 64)
+    pool = torch.full((3, 400, 4, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    Q, K, V, dO = inputs(heads, 400, 400, 9)
+    O = pool[1]
+    for q, k in (([0, 500, 100, 2 ** 30], [0, 100, 50, 9000]), ([-5, 20, 10, 400], [300, 200, 100, 0]), ([400, 400, 0, 7], [-9, -4, 3, 2 ** 31 - 1])):
+        qs, ks = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (q, k))
+        sh = B.PromptShape(3, 400, 400, *heads)
+        _, lse = B.prompt_attn(sh, Q, K, V, qs, ks, O=O, return_lse=True)
+        B.prompt_attn_bwd(sh, Q, K, V, O.clone(), torch.zeros_like(lse), dO, qs, ks, dQ=O)
+        torch.cuda.synchronize()
+        assert (pool[0] == 5).all() and (pool[2] == 5).all()
+
+
+def test_other_stream_and_replayed_graphs(B):
+    """On a side stream, and captured twice with one workspace: every replay equals the eager call on its inputs."""
+    heads, q_len, k_len = (8, 2, 64), [40, 3], [4000, 900]  # few rows on many keys: the forward uses its workspace, too
+    tq, tk = sum(q_len), sum(k_len)
+    sh = B.PromptShape(2, tq, tk, *heads)
+    qs, ks = R.starts(q_len).cuda(), R.starts(k_len).cuda()
+    assert B.prompt_workspace_bytes(sh, B.PROMPT_ATTN) > 0
+    ws = torch.empty(max(B.prompt_workspace_bytes(sh, c) for c in (B.PROMPT_ATTN, B.PROMPT_ATTN_BWD)), dtype=torch.uint8, device="cuda")
+    sets = [inputs(heads, tq, tk, s) for s in (1, 2)]
+    live = [t.clone() for t in sets[0]]
+    O, lse = torch.empty_like(live[0]), torch.empty((tq, heads[0]), device="cuda")
+    grads = [torch.empty_like(live[0]), torch.empty_like(live[1]), torch.empty_like(live[2])]
+
+    def forward():
+        B.prompt_attn(sh, *live[:3], qs, ks, O=O, lse=lse, workspace=ws)
+
+    def backward():
+        B.prompt_attn_bwd(sh, *live[:3], O, lse, live[3], qs, ks, workspace=ws, dQ=grads[0], dK=grads[1], dV=grads[2])
+
+    eager = []
+    for s in sets:
+        for dst, src in zip(live, s):
+            dst.copy_(src)
+        forward()
+        backward()
+        torch.cuda.synchronize()
+        eager.append([t.clone() for t in (O, lse, *grads)])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        forward()
+        backward()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((O, lse, *grads), eager[1]))
+    graphs = []
+    for step in (forward, backward):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            step()
+    for which in (1, 0, 0, 1):
+        for dst, src in zip(live, sets[which]):
+            dst.copy_(src)
+        for t in (O, lse, *grads):
+            t.fill_(1)
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((O, lse, *grads), eager[which]))

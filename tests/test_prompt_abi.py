@@ -1,0 +1,134 @@
+"""CPU-only checks of the entries for packed prompts and the paged cache: what they refuse, before anything is launched, and
+what their workspaces are."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2604_08077_amd import binding as B
+
+OK, EINVAL, EUNSUPPORTED, EWORKSPACE = 0, -1, -2, -3
+P = 1 << 20  # stands for a device address: 16-byte aligned, never read
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return B.load()
+
+
+def prompts(**kw):
+    c = dict(sequences=2, q_tokens=8, k_tokens=8, q_heads=4, kv_heads=2, head_dim=64, q_stride=0, k_stride=0, v_stride=0)
+    c.update(kw)
+    return B._CPrompts(*c.values())
+
+
+def cache(**kw):
+    c = dict(sequences=2, pages=4, page_size=16, table_pages=3, q_heads=4, kv_heads=2, head_dim=64, format=0)
+    c.update(kw)
+    return B._CCache(*c.values())
+
+
+BAD_HEADS = [(dict(q_heads=0), EINVAL), (dict(q_heads=3), EINVAL), (dict(kv_heads=-1), EINVAL), (dict(head_dim=96), EUNSUPPORTED)]
+BAD_PROMPTS = BAD_HEADS + [
+    (dict(sequences=0), EINVAL), (dict(q_tokens=-1), EINVAL), (dict(k_tokens=-1), EINVAL),
+    (dict(q_stride=255), EINVAL), (dict(q_stride=260), EINVAL), (dict(k_stride=64), EINVAL), (dict(v_stride=-8), EINVAL),
+    (dict(v_stride=(1 << 22) + 8), EUNSUPPORTED), (dict(q_tokens=1 << 30), EUNSUPPORTED), (dict(k_tokens=(1 << 30)), EUNSUPPORTED),
+    (dict(sequences=1 << 24), EUNSUPPORTED)]
+BAD_CACHES = BAD_HEADS + [
+    (dict(sequences=0), EINVAL), (dict(pages=0), EINVAL), (dict(page_size=0), EINVAL), (dict(table_pages=0), EINVAL),
+    (dict(format=2), EINVAL), (dict(page_size=24), EUNSUPPORTED), (dict(page_size=1 << 20, table_pages=1 << 11), EUNSUPPORTED),
+    (dict(pages=1 << 30), EUNSUPPORTED)]
+
+
+@pytest.mark.parametrize("kw,code", BAD_PROMPTS)
+def test_prompts_that_are_refused(lib, kw, code):
+    c, n = prompts(**kw), ctypes.c_size_t(0)
+    assert lib.adaspark_prompt_workspace_bytes(ctypes.byref(c), 0, 1, ctypes.byref(n)) == code
+    assert lib.adaspark_prompt_attn(ctypes.byref(c), P, P, P, P, P, 1, P, None, None, 0, None) == code
+    assert lib.adaspark_prompt_attn_bwd(ctypes.byref(c), P, P, P, P, P, P, P, P, 1, P, P, P, P, 1 << 40, None) == code
+
+
+@pytest.mark.parametrize("kw,code", BAD_CACHES)
+def test_caches_that_are_refused(lib, kw, code):
+    c, n = cache(**kw), ctypes.c_size_t(0)
+    assert lib.adaspark_decode_workspace_bytes(ctypes.byref(c), ctypes.byref(n)) == code
+    assert lib.adaspark_cache_write(ctypes.byref(c), 1, P, 0, P, 0, P, P, P, P, P, None, None, None) == code
+    assert lib.adaspark_cache_read(ctypes.byref(c), 1, P, P, P, P, None, None, P, P, None) == code
+    assert lib.adaspark_decode_attn(ctypes.byref(c), P, P, P, P, P, None, None, P, None, P, 1 << 40, None) == code
+
+
+def test_pointers_and_workspaces_that_are_refused(lib):
+    n = ctypes.c_size_t(0)
+    c = prompts()
+    good = [ctypes.byref(c), P, P, P, P, P, 1, P, None, None, 0, None]
+    for at, bad in ((0, None), (1, None), (1, P + 8), (2, None), (3, P + 2), (4, None), (5, P + 2), (7, None), (8, P + 4)):
+        args = list(good)
+        args[at] = bad
+        assert lib.adaspark_prompt_attn(*args) == EINVAL, at
+    # few rows on many keys: parts of rows, in a workspace
+    few = prompts(q_tokens=1, k_tokens=100000, sequences=1)
+    assert lib.adaspark_prompt_workspace_bytes(ctypes.byref(few), 0, 1, ctypes.byref(n)) == OK and n.value > 0
+    args = [ctypes.byref(few), *good[1:]]
+    assert lib.adaspark_prompt_attn(*args) == EWORKSPACE
+    args[9:11] = [P, n.value - 1]
+    assert lib.adaspark_prompt_attn(*args) == EWORKSPACE
+    args[9:11] = [P + 4, n.value]
+    assert lib.adaspark_prompt_attn(*args) == EWORKSPACE
+    assert lib.adaspark_prompt_workspace_bytes(ctypes.byref(c), 2, 1, ctypes.byref(n)) == EINVAL
+    assert lib.adaspark_prompt_workspace_bytes(ctypes.byref(c), 0, 1, None) == EINVAL
+    # the backward: outputs over inputs or each other, no workspace
+    size = 8 * 4 * 64 * 2
+    at = [P + i * 2 * size for i in range(9)]
+    bwd = lambda o, ws=P, wb=1 << 40: lib.adaspark_prompt_attn_bwd(  # noqa: E731
+        ctypes.byref(c), at[0], at[1], at[2], at[3], at[4], at[5], P, P, 1, *o, ws, wb, None)
+    for o in ((at[0], at[7], at[8]), (at[6], at[1] + 16, at[8]), (at[6], at[7], at[7] + 1024), (at[5], at[7], at[8]), (at[6], at[7], at[4])):
+        assert bwd(o) == EINVAL
+    assert bwd((at[6], at[7], at[8]), None, 0) == EWORKSPACE
+    assert bwd((at[6], at[7], None)) == EINVAL
+    # the cache: scales with a bf16 cache, none with an 8-bit one
+    c = cache()
+    assert lib.adaspark_cache_read(ctypes.byref(c), 1, P, P, P, P, P, P, P, P, None) == EINVAL
+    c8 = cache(format=1)
+    assert lib.adaspark_cache_read(ctypes.byref(c8), 1, P, P, P, P, P, None, P, P, None) == EINVAL
+    assert lib.adaspark_cache_write(ctypes.byref(c8), 1, P, 0, P, 0, P, P, P, P, P, None, P, None) == EINVAL
+    assert lib.adaspark_cache_write(ctypes.byref(c), -1, P, 0, P, 0, P, P, P, P, P, None, None, None) == EINVAL
+    assert lib.adaspark_cache_write(ctypes.byref(c), 1, P, 100, P, 0, P, P, P, P, P, None, None, None) == EINVAL
+    assert lib.adaspark_decode_workspace_bytes(ctypes.byref(c), None) == EINVAL
+    assert lib.adaspark_decode_workspace_bytes(ctypes.byref(c), ctypes.byref(n)) == OK and n.value > 0
+    assert lib.adaspark_decode_attn(ctypes.byref(c), P, P, P, P, P, None, None, P, None, None, 0, None) == EWORKSPACE
+
+
+def test_nothing_to_do_is_no_error(lib):
+    c, k = prompts(q_tokens=0, k_tokens=0), cache()
+    assert lib.adaspark_prompt_attn(ctypes.byref(c), None, None, None, P, P, 1, None, None, None, 0, None) == OK
+    assert lib.adaspark_prompt_attn_bwd(ctypes.byref(c), None, None, None, None, None, None, P, P, 1, None, None, None, P, 1 << 20, None) == OK
+    assert lib.adaspark_cache_write(ctypes.byref(k), 0, None, 0, None, 0, P, P, P, P, P, None, None, None) == OK
+    assert lib.adaspark_cache_read(ctypes.byref(k), 0, P, P, P, P, None, None, None, None, None) == OK
+
+
+def test_workspaces_follow_the_work():
+    size = lambda *a, call=B.PROMPT_ATTN: B.prompt_workspace_bytes(B.PromptShape(*a), call)  # noqa: E731
+    assert size(1, 32000, 32000, 28, 4, 128) == 0                  # enough rows for every CU
+    assert 0 < size(2, 80, 40000, 28, 4, 128) < 128 << 20
+    rows = 2 * 4 * 32000 * 28
+    assert rows <= size(1, 32000, 32000, 28, 4, 128, call=B.PROMPT_ATTN_BWD) < 1 << 30
+    assert B.decode_workspace_bytes(B.CacheShape(4096, 8, 16, 4, 8, 2, 64)) == 0
+
+
+def test_tensors_that_are_refused():
+    sh = B.PromptShape(1, 4, 4, 4, 2, 64)
+    Q, K = torch.zeros(4, 4, 64, dtype=torch.bfloat16), torch.zeros(4, 2, 64, dtype=torch.bfloat16)
+    start = torch.tensor([0, 4], dtype=torch.int32)
+    with pytest.raises(ValueError, match="GPU tensor"):
+        B.prompt_attn(sh, Q, K, K, start)
+    csh = B.CacheShape(1, 2, 16, 2, 4, 2, 64)
+    c = B.Cache(*(torch.zeros(2, 2, 16, 64, dtype=torch.bfloat16) for _ in range(2)))
+    table, lengths = torch.zeros(1, 2, dtype=torch.int32), torch.ones(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="GPU tensor"):
+        B.cache_write(csh, K, K, start, c, table, lengths)
+    with pytest.raises(ValueError, match="GPU tensor"):
+        B.cache_read(csh, c, table, start, 4)
+    with pytest.raises(ValueError, match="GPU tensor"):
+        B.decode_attn(csh, Q[:1], c, table, lengths)
+    with pytest.raises(B.AdasparkError):
+        B.decode_workspace_bytes(B.CacheShape(1, 2, 16, 2, 4, 2, 64, "int4"))
