@@ -12,7 +12,7 @@
 // -lse * sqrt(D) and those of dP from -delta, which prompt_prep_kernel leaves per row.
 // Score products are exact; p and dS are rounded to bf16 as operands of the other products, sums are fp32.
 //
-// Where few key blocks have long walks, a walk is cut into spans of equal length, a workgroup each, which leave fp32 sums in the
+// Where few key blocks have long walks, a walk is cut into spans, a workgroup each, which leave fp32 sums in the
 // workspace; prompt_reduce_kernel adds them in their order.
 #include <algorithm>
 
@@ -35,31 +35,50 @@ struct PromptBwd {
     static_assert(BYTES <= 160 * 1024, "LDS of one CU");
 };
 
-// ---- the spans of the dK/dV kernel
+// ---- the spans of the dK/dV kernel: row tiles of a workgroup.  How long they are follows from the lengths, which the device knows
+// (span_tiles); how many a block may have at most, and with it the workspace, from the tokens of all sequences.
 struct PromptSpans {
     long long blocks;  // bound of the key blocks per KV head
-    int tiles;         // row tiles of a span
     int most;          // spans of a block at most
 };
+constexpr int SPAN_MIN = 4;        // tiles; a span's sums are written and read again, about as much time as two take
+constexpr int SPAN_ITEMS = 768;    // workgroups that the tiles of all blocks are to be shared out to, three per CU
 static long long key_block_bound(const PromptGeom &g) { return (long long)g.Tk / PB_BLOCK + g.B; }
 __device__ __forceinline__ int key_block_id(int s, int k0, int j) { return k0 / PB_BLOCK + s + j; }
 
-// What is known here are the tokens of all sequences, so the cut is that of one sequence of them all: spans of a length
-// that gives about three workgroups per CU, eight tiles at least (a span's sums are written and read again, about as much time as two tiles
-// take); shorter sequences then have fewer spans, or one, which writes its gradients itself.
 static PromptSpans prompt_spans(const PromptGeom &g)
 {
     PromptSpans s;
     s.blocks = key_block_bound(g);
-    const long long tiles = ((long long)g.Tq * g.G + 63) / 64;
-    const long long total = s.blocks * g.Hkv * tiles / (g.causal ? 2 : 1);
-    s.tiles = (int)std::max(8ll, std::min((total + 767) / 768, std::max(1ll, tiles)));
-    s.most = (int)std::max(1ll, (tiles + s.tiles - 1) / s.tiles);
-    if (s.most == 1) s.tiles = (int)std::max(1ll, tiles);
+    const long long tiles = ((long long)g.Tq * g.G + 63) / 64;  // of the longest walk that there can be
+    const long long span = std::max((long long)SPAN_MIN, s.blocks * g.Hkv * tiles / (g.causal ? 2 : 1) / SPAN_ITEMS);
+    s.most = (int)std::max(1ll, (tiles + span - 1) / span);
     return s;
 }
 
+// Tiles of a span: those of all blocks over SPAN_ITEMS, but no walk in more than `most`.  Worked out by one wavefront.
+__device__ __forceinline__ int span_tiles(const PromptGeom &g, int most)
+{
+    float total = 0.f;  // rows of all walks of a KV head
+    int longest = 0;
+    for (int s = threadIdx.x & 63; s < g.B; s += 64) {
+        const PromptSeq p = prompt_seq(g, s);
+        const long long rows = (long long)p.n * g.G, nb = (p.m + PB_BLOCK - 1) / PB_BLOCK, off = p.m - p.n;
+        // block j's walk begins at row G * max(0, 256 j - off)
+        const long long z = g.causal ? min(nb, max(0ll, off / PB_BLOCK + (off >= 0 ? 1 : 0))) : nb, rest = nb - z;
+        total += (float)nb * (float)rows - (float)g.G * ((float)(PB_BLOCK * (z + nb - 1)) * 0.5f - (float)off) * (float)rest;
+        if (p.m > 0) longest = max(longest, (int)((rows - (g.causal ? min(rows, max(0ll, -off) * g.G) : 0) + 63) / 64));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        total += __shfl_xor(total, d, 64);
+        longest = max(longest, __shfl_xor(longest, d, 64));
+    }
+    return max(max(SPAN_MIN, (longest + most - 1) / most), (int)min(total * (float)g.Hkv / (64.f * SPAN_ITEMS), 1e9f));
+}
+
 struct PromptBwdWorkspace {
+    int *span;            // tiles of a span
     float *lse2, *delta;  // [Tq * Hq + 1]: entry [Tq * Hq] belongs to the rows that pad a tile: -inf, 0
     float *part;          // [Hkv][blocks][most][2 (dV, dK)][256 x D] in MFMA output order
     size_t bytes;
@@ -71,22 +90,28 @@ static PromptBwdWorkspace bwd_workspace_of(const PromptGeom &g, int D, void *ws)
     const size_t rows = up(((size_t)g.Tq * g.Hq + 1) * 4);
     unsigned char *p = static_cast<unsigned char *>(ws);
     PromptBwdWorkspace w;
+    w.span = reinterpret_cast<int *>(p);
+    p += 256;
     w.lse2 = reinterpret_cast<float *>(p);
     w.delta = reinterpret_cast<float *>(p + rows);
     w.part = reinterpret_cast<float *>(p + 2 * rows);
-    w.bytes = 2 * rows + (s.most > 1 ? (size_t)g.Hkv * s.blocks * s.most * 2 * PB_BLOCK * D * 4 : 0);
+    w.bytes = 256 + 2 * rows + (s.most > 1 ? (size_t)g.Hkv * s.blocks * s.most * 2 * PB_BLOCK * D * 4 : 0);
     return w;
 }
 size_t prompt_bwd_workspace_bytes(const PromptGeom &g, int D) { return bwd_workspace_of(g, D, nullptr).bytes; }
 
 // Start values of every row: 256 / (D / 8) rows to a workgroup, D / 8 lanes to a row.  A row without keys (log-sum-exp -inf) gets
-// no part in anything.
+// no part in anything.  The first workgroup's first wavefront also leaves the length of a span.
 template <int D>
-__global__ __launch_bounds__(256) void prompt_prep_kernel(long long rows, const uint16_t *__restrict__ O, const uint16_t *__restrict__ dO,
+__global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most, int *__restrict__ span, long long rows, const uint16_t *__restrict__ O, const uint16_t *__restrict__ dO,
                                                           const float *__restrict__ lse, float *__restrict__ lse2,
                                                           float *__restrict__ delta)
 {
     constexpr int CPR = D / 8;
+    if (blockIdx.x == 0 && threadIdx.x < 64) {
+        const int tiles = span_tiles(g, most);
+        if (threadIdx.x == 0) *span = tiles;
+    }
     const long long r = ((long long)blockIdx.x * 256 + threadIdx.x) / CPR;
     const int col = threadIdx.x % CPR;
     float part = 0.f;
@@ -272,7 +297,7 @@ __device__ __forceinline__ int key_blocks(int n, int m, int G, int causal, int t
 
 template <int D>
 __global__ __launch_bounds__(PB_THREADS) void prompt_dkv_kernel(PromptGeom g, int per_head, PromptSpans cut,
-                                                                const uint16_t *__restrict__ Q, const uint16_t *__restrict__ K,
+                                                                const int *__restrict__ span_p, const uint16_t *__restrict__ Q, const uint16_t *__restrict__ K,
                                                                 const uint16_t *__restrict__ V, const uint16_t *__restrict__ dO,
                                                                 const float *__restrict__ lse2p, const float *__restrict__ deltap,
                                                                 float *__restrict__ partial, uint16_t *__restrict__ dK,
@@ -286,7 +311,7 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dkv_kernel(PromptGeom g, in
 
     int kv, slot, seq, j;
     if (!head_slot(blockIdx.x, g.Hkv, per_head, kv, slot)) return;
-    const int span = slot % cut.most;
+    const int span = slot % cut.most, span_len = *span_p;
     if (!prompt_block(g, slot / cut.most, (int)(((long long)g.Tq * g.G + 63) / 64),
                       [&](int n, int m, int t) { return key_blocks(n, m, g.G, g.causal, t); }, seq, j))
         return;
@@ -296,9 +321,9 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dkv_kernel(PromptGeom g, in
     const int rows = p.n * g.G, off = p.m - p.n;
     auto first_row = [&](int key) { return g.causal ? (int)min((long long)rows, max(0ll, (long long)key - off) * g.G) : 0; };  // that attends it
     const int first = first_row(j * PB_BLOCK);
-    const int all = (rows - first + 63) / 64, spans = max(1, (all + cut.tiles - 1) / cut.tiles);
+    const int all = (rows - first + 63) / 64, spans = max(1, (all + span_len - 1) / span_len);
     if (span >= spans) return;
-    const int row0 = first + span * cut.tiles * 64, ntiles = min(cut.tiles, all - span * cut.tiles);
+    const int row0 = first + span * span_len * 64, ntiles = min(span_len, all - span * span_len);
 
     const int key0 = j * PB_BLOCK + wave * 32;
     const bool busy = key0 < p.m;
@@ -470,7 +495,7 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dkv_kernel(PromptGeom g, in
 // The spans' sums of a key block, added in their order: eight workgroups to a block, one for each wavefront's keys; NS * DT * 64
 // places in MFMA output order.
 template <int D>
-__global__ __launch_bounds__(256) void prompt_reduce_kernel(PromptGeom g, PromptSpans cut, const float *__restrict__ partial,
+__global__ __launch_bounds__(256) void prompt_reduce_kernel(PromptGeom g, PromptSpans cut, const int *__restrict__ span_p, const float *__restrict__ partial,
                                                             uint16_t *__restrict__ dK, uint16_t *__restrict__ dV)
 {
     constexpr int NS = 2, DT = D / 16;
@@ -485,7 +510,7 @@ __global__ __launch_bounds__(256) void prompt_reduce_kernel(PromptGeom g, Prompt
     const int j = id - key_block_id(lo, p.k0, 0);
     if (j < 0 || j * (long long)PB_BLOCK >= p.m) return;
     const long long rows = (long long)p.n * g.G, first = g.causal ? min(rows, max(0ll, (long long)j * PB_BLOCK - (p.m - p.n)) * g.G) : 0;
-    const int all = (int)((rows - first + 63) / 64), spans = (all + cut.tiles - 1) / cut.tiles;
+    const int span_len = *span_p, all = (int)((rows - first + 63) / 64), spans = (all + span_len - 1) / span_len;
     if (spans <= 1) return;
     const f32x4 *from = reinterpret_cast<const f32x4 *>(partial) + ((size_t)kv * cut.blocks + id) * cut.most * (2 * PB_BLOCK * D / 4) + wave * (NS * DT * 64);
     const float c = 1.0f / sqrtf((float)D);
@@ -516,14 +541,14 @@ static hipError_t launch_bwd(const PromptGeom &g, const uint16_t *Q, const uint1
     if (e == hipSuccess) e = opted_kv.ensure(reinterpret_cast<const void *>(&prompt_dkv_kernel<D>), C::BYTES);
     if (e != hipSuccess) return e;
     const long long rows = (long long)g.Tq * g.Hq, per = 256 / (D / 8);
-    hipLaunchKernelGGL((prompt_prep_kernel<D>), dim3((unsigned)((rows + 1 + per - 1) / per)), dim3(256), 0, st, rows, O, dO, lse, w.lse2,
-                       w.delta);
+    hipLaunchKernelGGL((prompt_prep_kernel<D>), dim3((unsigned)((rows + 1 + per - 1) / per)), dim3(256), 0, st, g, cut.most, w.span, rows, O, dO,
+                       lse, w.lse2, w.delta);
     if (g.Tk > 0) {
         const int keys = (int)cut.blocks * cut.most;
-        hipLaunchKernelGGL((prompt_dkv_kernel<D>), dim3(head_grid(g.Hkv, keys)), dim3(PB_THREADS), C::BYTES, st, g, keys, cut, Q, K, V, dO,
+        hipLaunchKernelGGL((prompt_dkv_kernel<D>), dim3(head_grid(g.Hkv, keys)), dim3(PB_THREADS), C::BYTES, st, g, keys, cut, w.span, Q, K, V, dO,
                            w.lse2, w.delta, w.part, dK, dV);
         if (cut.most > 1)
-            hipLaunchKernelGGL((prompt_reduce_kernel<D>), dim3((unsigned)(cut.blocks * g.Hkv * 8)), dim3(256), 0, st, g, cut, w.part, dK, dV);
+            hipLaunchKernelGGL((prompt_reduce_kernel<D>), dim3((unsigned)(cut.blocks * g.Hkv * 8)), dim3(256), 0, st, g, cut, w.span, w.part, dK, dV);
     }
     if (g.Tq > 0) {
         const int blocks = (int)row_block_bound(g, PB_BLOCK);
