@@ -377,7 +377,7 @@ int adaspark_ffn_sparse(const adaspark_shape *shape, const adaspark_ffn_dims *di
  *                   shared out to several workgroups; may then be NULL
  * Score products are exact in fp32 and the log-sum-exp is that of fp32 weights; the weights are rounded to bf16 (off by up to 2^-8 of each) for their
  * products with V.  K and V of a sequence have to be finite: a row may multiply the V of a key that it does not attend by a weight of 0.
- * Limits: head_dim in {64, 128}; q_tokens*q_heads and k_tokens*kv_heads < 2^31; strides multiples of 8 up to 2^22, and
+ * Limits: head_dim in {64, 128}; q_heads/kv_heads <= 128; q_tokens*q_heads and k_tokens*kv_heads < 2^31, either number of tokens <= 2^30; strides multiples of 8 up to 2^22, and
  * at least heads*head_dim (otherwise ADASPARK_EINVAL).
  */
 typedef struct {

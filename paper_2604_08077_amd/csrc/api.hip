@@ -83,6 +83,8 @@ int check_prompts(const adaspark_prompts *p)
     for (const auto &x : {std::make_pair(p->q_stride, p->q_heads), std::make_pair(p->k_stride, p->kv_heads), std::make_pair(p->v_stride, p->kv_heads)})
         if ((rc = check_stride(x.first, x.second, p->head_dim)) != ADASPARK_OK) return rc;
     if ((long long)p->q_tokens * p->q_heads >= (1ll << 31) || (long long)p->k_tokens * p->kv_heads >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
+    if (p->q_heads / p->kv_heads > PROMPT_MAX_GROUP) return ADASPARK_EUNSUPPORTED;
+    if (p->q_tokens > (1 << 30) || p->k_tokens > (1 << 30)) return ADASPARK_EUNSUPPORTED;
     // the workgroups of a launch, with room for spans and parts
     if (((long long)p->q_tokens * (p->q_heads / p->kv_heads) / 256 + p->sequences) * p->kv_heads >= (1ll << 24)) return ADASPARK_EUNSUPPORTED;
     if (((long long)p->k_tokens / 256 + p->sequences) * p->kv_heads >= (1ll << 24)) return ADASPARK_EUNSUPPORTED;

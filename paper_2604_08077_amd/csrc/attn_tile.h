@@ -29,6 +29,13 @@ __device__ __forceinline__ void dma_1k_s(uint32_t lds_addr, const void *sbase, u
                  : "memory", "m0");
 }
 
+// The same with 4 bytes to a lane: 256 bytes.
+__device__ __forceinline__ void dma_256_s(uint32_t lds_addr, const void *sbase, uint32_t voff)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_addr), "v"(voff), "s"(sbase)
+                 : "memory", "m0");
+}
+
 // A wave-uniform pointer moved into scalar registers, as dma_1k_s wants its base (readfirstlane returns a signed
 // int: each half is widened through uint32_t, or a low half with bit 31 set would smear ones over the high half).
 __device__ __forceinline__ const void *uniform_ptr(const void *p)

@@ -12,7 +12,7 @@ namespace adaspark {
 struct PromptGeom {
     const int32_t *q_start, *k_start;     // [B + 1]
     int B, Tq, Tk, Hq, Hkv, G, causal;
-    uint32_t gmul, gshift;                // division of a row number by G (token_of_row)
+    uint32_t gmul, gshift, gnear;         // division of a row number by G (token_of_row, token_of_near_row)
     long long qs, ks, vs;                 // elements from one token of Q, K, V to the next
 };
 
@@ -33,6 +33,7 @@ inline PromptGeom make_prompt_geom(const adaspark_prompts &p, const int32_t *q_s
     while ((1ll << s) < g.G) ++s;
     g.gmul = g.G == 1 ? 0u : (uint32_t)((1ull << (31 + s)) / (unsigned long long)g.G + 1);
     g.gshift = (uint32_t)s - 1;
+    g.gnear = 65536u / (uint32_t)g.G + 1;
     g.causal = causal != 0;
     g.qs = p.q_stride ? p.q_stride : (long long)p.q_heads * p.head_dim;
     g.ks = p.k_stride ? p.k_stride : (long long)p.kv_heads * p.head_dim;
@@ -45,6 +46,10 @@ __device__ __forceinline__ int token_of_row(const PromptGeom &g, int row)
 {
     return g.G == 1 ? row : (int)(__umulhi((uint32_t)row, g.gmul) >> g.gshift);
 }
+
+// The same for 0 <= x < 64 + G, G <= PROMPT_MAX_GROUP: gnear * G is over 65536 by at most G, and x * G < 65536.
+constexpr int PROMPT_MAX_GROUP = 128;
+__device__ __forceinline__ uint32_t token_of_near_row(const PromptGeom &g, uint32_t x) { return __umul24(x, g.gnear) >> 16; }
 
 // A sequence: its first query and key token, and how many.  Starts that do not fit the tensors are cut to them: whatever the arrays hold,
 // nothing outside is touched.
@@ -61,100 +66,126 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptGeom &g, int s)
     return p;
 }
 
-// Work is dealt out longest first: a launch ends when its last workgroup does, and a long walk begun late is the tail.  The
-// lengths are on the device, so every wavefront finds its own: the w-th longest block, lengths told apart in half octaves
-// (0, 1, 2, 3, 4, 6, 8, 12, ... tiles).  `count(n, m, t)`: blocks of a sequence (n queries, m keys) with a walk of at least t tiles, t = 0: all; they are
-// the sequence's last ones (`from_end`) or first ones.  Sequences beyond 512 are dealt out 512 at a time.
-constexpr int PROMPT_SEQS = 512;
+__device__ __forceinline__ PromptSeq seq_uniform(const PromptSeq &p)
+{
+    return {__builtin_amdgcn_readfirstlane(p.q0), __builtin_amdgcn_readfirstlane(p.n), __builtin_amdgcn_readfirstlane(p.k0),
+            __builtin_amdgcn_readfirstlane(p.m)};
+}
+
+// Inclusive scan over a wavefront's lanes, without LDS: within rows of 16, then each row's sum carried on.
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
+
+// What a workgroup does follows from lengths that only the device knows, so every wavefront finds its own work: the w-th block of
+// all.  A wavefront's lanes hold the lengths of 512 sequences, eight each; beyond, sequences are taken 512 at a time.
+// count(n, m, t): blocks of a sequence (n queries, m keys) with a walk of at least t tiles (t = 0: all of them); they are the
+// sequence's last ones (rows) or first ones (keys), and are numbered from the longest.
+constexpr int PROMPT_SEQS = 512, PROMPT_CHUNKS = PROMPT_SEQS / 64;
+struct PromptLengths {
+    int q0[PROMPT_CHUNKS], n[PROMPT_CHUNKS], k0[PROMPT_CHUNKS], m[PROMPT_CHUNKS];
+    int s0, chunks;
+};
+__device__ __forceinline__ PromptLengths prompt_lengths(const PromptGeom &g, int s0)
+{
+    PromptLengths l;
+    l.s0 = s0;
+    l.chunks = (min(g.B - s0, PROMPT_SEQS) + 63) >> 6;
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int c = 0; c < PROMPT_CHUNKS; ++c) {
+        PromptSeq p = {0, 0, 0, 0};
+        if (c < l.chunks && s0 + 64 * c + lane < g.B) p = prompt_seq(g, s0 + 64 * c + lane);
+        l.q0[c] = p.q0;
+        l.n[c] = p.n;
+        l.k0[c] = p.k0;
+        l.m[c] = p.m;
+    }
+    return l;
+}
+
+struct PromptBlock {
+    PromptSeq p;
+    int seq, block;  // block: counted from the sequence's longest
+};
+template <typename Count>
+__device__ __forceinline__ int blocks_from(const PromptLengths &l, int t, Count count)
+{
+    int x = 0;
+#pragma unroll
+    for (int c = 0; c < PROMPT_CHUNKS; ++c)
+        if (c < l.chunks) x += count(l.n[c], l.m[c], t);
+    return wave_total(x);
+}
+// The r-th of the blocks with a walk of t0 .. t1 - 1 tiles (t1 < 0: or more).
+template <typename Count>
+__device__ __forceinline__ PromptBlock nth_block(const PromptLengths &l, int r, int t0, int t1, Count count)
+{
+    PromptBlock b = {{0, 0, 0, 0}, -1, 0};
+#pragma unroll
+    for (int c = 0; c < PROMPT_CHUNKS; ++c) {
+        if (c >= l.chunks || b.seq >= 0) continue;
+        const int longer = t1 < 0 ? 0 : count(l.n[c], l.m[c], t1), mine = count(l.n[c], l.m[c], t0) - longer, incl = wave_scan(mine);
+        const unsigned long long hit = __ballot(r < incl);
+        if (hit != 0ull) {
+            const int src = __builtin_amdgcn_readfirstlane(__ffsll(hit) - 1);
+            b.seq = l.s0 + 64 * c + src;
+            b.block = __builtin_amdgcn_readlane(longer, src) + r - __builtin_amdgcn_readlane(incl - mine, src);
+            b.p = {__builtin_amdgcn_readlane(l.q0[c], src), __builtin_amdgcn_readlane(l.n[c], src), __builtin_amdgcn_readlane(l.k0[c], src),
+                   __builtin_amdgcn_readlane(l.m[c], src)};
+        }
+        r -= __builtin_amdgcn_readlane(incl, 63);
+    }
+    return b;
+}
+
+// Blocks dealt out longest first -- a launch ends when its last workgroup does, and a long walk begun late is the tail --, lengths
+// told apart in half octaves (0, 1, 2, 3, 4, 6, 8, 12, ... tiles).  The w-th block; seq -1: there is none.
 __device__ __forceinline__ int walk_level(int b)  // the b-th length
 {
     return b < 2 ? b : (2 + (b & 1)) << ((b - 2) >> 1);
 }
-
-__device__ __forceinline__ int wave_total(int x)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
-    return __builtin_amdgcn_readfirstlane(x);
-}
-
-// The w-th block: its sequence, and its number among the sequence's blocks counted from the longest.  false: there is none.
 template <typename Count>
-__device__ __forceinline__ bool prompt_block(const PromptGeom &g, int w, int most_tiles, Count count, int &seq, int &block)
+__device__ __forceinline__ PromptBlock longest_first(const PromptGeom &g, int w, int most_tiles, Count count)
 {
-    const int lane = threadIdx.x & 63;
+    int top = 1;
+    while (walk_level(top) <= most_tiles) ++top;  // (no block is that long)
     for (int s0 = 0; s0 < g.B; s0 += PROMPT_SEQS) {
-        const int chunks = (min(g.B - s0, PROMPT_SEQS) + 63) >> 6;
-        int n[PROMPT_SEQS / 64], m[PROMPT_SEQS / 64];
-#pragma unroll
-        for (int c = 0; c < PROMPT_SEQS / 64; ++c) {
-            n[c] = m[c] = 0;
-            if (c < chunks && s0 + 64 * c + lane < g.B) {
-                const PromptSeq p = prompt_seq(g, s0 + 64 * c + lane);
-                n[c] = p.n;
-                m[c] = p.m;
-            }
-        }
-        auto total = [&](int t) -> int {
-            int x = 0;
-#pragma unroll
-            for (int c = 0; c < PROMPT_SEQS / 64; ++c)
-                if (c < chunks) x += count(n[c], m[c], t);
-            return wave_total(x);
-        };
-        const int all = total(0);
+        const PromptLengths l = prompt_lengths(g, s0);
+        const int all = blocks_from(l, 0, count);
         if (w >= all) {
             w -= all;
             continue;
         }
-        // the highest level with more than w blocks
-        int lo = 0, hi = 1;
-        while (walk_level(hi) <= most_tiles) ++hi;  // (no block is that long)
+        int lo = 0, hi = top, above = 0;  // the highest level with more than w blocks, and the blocks beyond it
         while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (total(walk_level(mid)) > w) lo = mid;
-            else hi = mid;
+            const int mid = (lo + hi) >> 1, x = blocks_from(l, walk_level(mid), count);
+            if (x > w) lo = mid;
+            else hi = mid, above = x;
         }
-        const int above = walk_level(hi) <= most_tiles ? total(walk_level(hi)) : 0;
-        int r = w - above;
-        for (int c = 0; c < chunks; ++c) {
-            int nn = 0, mm = 0;
-#pragma unroll
-            for (int k = 0; k < PROMPT_SEQS / 64; ++k)
-                if (k == c) nn = n[k], mm = m[k];
-            const int longer = walk_level(hi) <= most_tiles ? count(nn, mm, walk_level(hi)) : 0;
-            const int mine = count(nn, mm, walk_level(lo)) - longer;
-            int incl = mine;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int up = __shfl_up(incl, d, 64);
-                if (lane >= d) incl += up;
-            }
-            const unsigned long long b = __ballot(r < incl);
-            if (b != 0ull) {
-                const int src = __builtin_amdgcn_readfirstlane(__ffsll(b) - 1);
-                seq = s0 + 64 * c + src;
-                block = __builtin_amdgcn_readlane(longer, src) + r - (__builtin_amdgcn_readlane(incl, src) - __builtin_amdgcn_readlane(mine, src));
-                return true;
-            }
-            r -= __builtin_amdgcn_readlane(incl, 63);
-        }
-        return false;  // (not reached: the counts add up)
+        return nth_block(l, w - above, walk_level(lo), hi == top ? -1 : walk_level(hi), count);
     }
-    return false;
+    return {{0, 0, 0, 0}, -1, 0};
 }
 
 // Blocks of R rows of a sequence and KV head whose walk over the keys has at least t tiles of 64; the last blocks walk farthest.
 template <int R>
 __device__ __forceinline__ int row_blocks(int n, int m, int G, int causal, int t)
 {
-    const long long rows = (long long)n * G;
-    const int nb = (int)((rows + R - 1) / R);
+    const int nb = (int)(((long long)n * G + R - 1) / R);
     if (t == 0) return nb;
-    const long long keys = 64ll * (t - 1);  // a walk of t tiles needs more than so many
+    const int keys = 64 * (t - 1);  // a walk of t tiles needs more than so many
     if (!causal) return m > keys ? nb : 0;
-    const long long first = max(0ll, keys - (m - n)) * G;  // the first row that reaches that far
-    return first < rows ? nb - (int)(first / R) : 0;
+    const int first = max(0, keys - (m - n));  // the first token that reaches that far
+    return first < n ? nb - first * G / R : 0;
 }
 
 // Workgroups per KV head that hold every block of R rows, however the tokens are shared out.

@@ -19,13 +19,12 @@
 
 namespace adaspark {
 
-template <int D>
+template <int D, int WAVES>
 struct Prompt {
-    static constexpr int WAVES = 8;
     static constexpr int THREADS = 64 * WAVES;
     static constexpr int NS = 2;
     static constexpr int ROWS = 16 * NS * WAVES;
-    static constexpr int NST = 3;  // LDS stages of K and of V
+    static constexpr int NST = WAVES == 8 ? 3 : 2;  // LDS stages of K and of V
     static constexpr int PF = 4;   // operand loads in flight ahead of the MFMAs
     static constexpr int TILE = KEY_TILE * D * 2;
     static constexpr int CPR = D / 8;              // 16-byte chunks of a row
@@ -35,11 +34,10 @@ struct Prompt {
     static constexpr int BYTES = 2 * NST * TILE;
     static_assert(BYTES <= 160 * 1024, "LDS of one CU");
 };
-constexpr int PROMPT_ROWS = Prompt<64>::ROWS;
 constexpr float LN2 = 0.69314718055994530942f;
 
-// A part's result: O unnormalised, fp32 [256 rows][D], then (m, l) of each row (m in base 2).
-__host__ __device__ inline size_t prompt_part_floats(int D) { return (size_t)PROMPT_ROWS * (D + 2); }
+// A part's result: O unnormalised, fp32 [rows][D], then (m, l) of each row (m in base 2).
+__host__ __device__ inline size_t prompt_part_floats(int rows, int D) { return (size_t)rows * (D + 2); }
 
 template <int KEEP>
 __device__ __forceinline__ void stage_barrier()
@@ -47,29 +45,28 @@ __device__ __forceinline__ void stage_barrier()
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(KEEP) : "memory");
 }
 
-template <int D, bool SPLIT>
-__global__ __launch_bounds__(512) void prompt_attn_kernel(PromptGeom g, int per_head, int parts, const uint16_t *__restrict__ Q,
+template <int D, int WAVES, bool SPLIT>
+__global__ __launch_bounds__(64 * WAVES, 2) void prompt_attn_kernel(PromptGeom g, int per_head, int parts, const uint16_t *__restrict__ Q,
                                                           const uint16_t *__restrict__ K, const uint16_t *__restrict__ V,
                                                           uint16_t *__restrict__ O, float *__restrict__ lse,
                                                           float *__restrict__ partial)
 {
-    using C = Prompt<D>;
+    using C = Prompt<D, WAVES>;
     constexpr int NS = C::NS, KSTEPS = D / 32, DT = D / 16, PF = C::PF;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
 
     const int lane = threadIdx.x & 63, n16 = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bool set_y = wave >= 4;
+    const bool set_y = WAVES == 8 && wave >= 4;
 
-    int kv, slot, seq, blk;
+    int kv, slot;
     if (!head_slot(blockIdx.x, g.Hkv, per_head, kv, slot)) return;
     const int part = SPLIT ? slot % parts : 0;
-    if (!prompt_block(g, SPLIT ? slot / parts : slot, (g.Tk + KEY_TILE - 1) / KEY_TILE,
-                      [&](int n, int m, int t) { return row_blocks<C::ROWS>(n, m, g.G, g.causal, t); }, seq, blk))
-        return;
-    seq = __builtin_amdgcn_readfirstlane(seq);
-    PromptSeq p = prompt_seq(g, seq);
-    const int rows = p.n * g.G, i = (rows - 1) / C::ROWS - blk, row0 = i * C::ROWS;
+    const PromptBlock b = longest_first(g, SPLIT ? slot / parts : slot, (g.Tk + KEY_TILE - 1) / KEY_TILE,
+                                        [&](int n, int m, int t) { return row_blocks<C::ROWS>(n, m, g.G, g.causal, t); });
+    if (b.seq < 0) return;
+    const PromptSeq p = b.p;
+    const int rows = p.n * g.G, i = (rows - 1) / C::ROWS - b.block, row0 = i * C::ROWS;
     auto reach_of = [&](int row) { return g.causal ? p.m - p.n + token_of_row(g, row) : p.m - 1; };  // the last key that a row attends
     auto tiles_to = [&](int row) { return max(0, reach_of(min(row, rows - 1)) / KEY_TILE + (reach_of(min(row, rows - 1)) >= 0 ? 1 : 0)); };
 
@@ -146,18 +143,25 @@ __global__ __launch_bounds__(512) void prompt_attn_kernel(PromptGeom g, int per_
         for (int e = 0; e < DT; ++e) oacc[s][e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // Slot t: K(t) and V(t-1) have landed, K(t+1) and V(t) may be in flight, K(t+2) and V(t+1) are started into the stages that fell
-    // free (as in attn_walk.hip).
-    int kst = 0;  // stage of K(t); V(t-1) sits in stage (kst + 2) % 3
+    // Slot t works on K(t) and V(t-1).  Three stages: K(t+1) and V(t) may be in flight when it opens, K(t+2) and V(t+1) are started into
+    // the stages that fell free (as in attn_walk.hip).  Two: K(t+1) and V(t) are started when it opens, and waited for at the next.
+    int kst = 0;  // stage of K(t); V(t-1) sits in the one before
+    auto before = [](int st) { return st == 0 ? C::NST - 1 : st - 1; };
+    auto after = [](int st) { return st == C::NST - 1 ? 0 : st + 1; };
     auto open_slot = [&](int t) __attribute__((always_inline)) {
-        if (t > 0 && t + 1 < ntiles) stage_barrier<2 * C::DMA>();
-        else stage_barrier<0>();
-        const int st_v = kst == 0 ? 2 : kst - 1, st_n = kst == 2 ? 0 : kst + 1;
-        if (t + 1 < ntiles) issue_v(t + 1, st_n);
-        if (t + 2 < ntiles) issue_k(t + 2, st_v);
+        if (C::NST == 3) {
+            if (t > 0 && t + 1 < ntiles) stage_barrier<2 * C::DMA>();
+            else stage_barrier<0>();
+            if (t + 1 < ntiles) issue_v(t + 1, after(kst));
+            if (t + 2 < ntiles) issue_k(t + 2, before(kst));
+        } else {
+            stage_barrier<0>();
+            if (t > 0 && t < ntiles) issue_v(t, kst);
+            if (t + 1 < ntiles) issue_k(t + 1, after(kst));
+        }
     };
     auto next_slot = [&](int t) __attribute__((always_inline)) {
-        kst = kst == 2 ? 0 : kst + 1;
+        kst = after(kst);
         open_slot(t);
     };
 
@@ -176,7 +180,7 @@ __global__ __launch_bounds__(512) void prompt_attn_kernel(PromptGeom g, int per_
     auto products = [&](auto pv, auto qk) __attribute__((always_inline)) {
         constexpr bool PV = decltype(pv)::value, QK = decltype(qk)::value;
         constexpr int RV = PV ? 2 * DT : 0, R = RV + (QK ? 4 * KSTEPS : 0);
-        const uint32_t kt = nat0 + (uint32_t)(kst * C::TILE), vt = tr0 + (uint32_t)((kst == 0 ? 2 : kst - 1) * C::TILE);
+        const uint32_t kt = nat0 + (uint32_t)(kst * C::TILE), vt = tr0 + (uint32_t)(before(kst) * C::TILE);
         bf16x8 ring[PF];
         auto operand = [&](int r) __attribute__((always_inline)) {
             return r < RV ? v_operand(vt, r / DT, r % DT) : k_operand(kt, (r - RV) / 4, (r - RV) % 4);
@@ -279,7 +283,7 @@ __global__ __launch_bounds__(512) void prompt_attn_kernel(PromptGeom g, int per_
     if (ntiles > 0) {
         issue_k(0, 0);
         issue_v(0, 0);
-        if (ntiles > 1) issue_k(1, 1);
+        if (C::NST == 3 && ntiles > 1) issue_k(1, 1);
     }
     const std::true_type yes;
     const std::false_type no;
@@ -314,7 +318,7 @@ __global__ __launch_bounds__(512) void prompt_attn_kernel(PromptGeom g, int per_
         const float l = quad_sum(l_run[s]);
         if (!valid[s]) continue;
         if (SPLIT) {
-            float *out = partial + (((size_t)kv * per_head / parts + row_block_id(g, C::ROWS, seq, p.q0, i)) * parts + part) * prompt_part_floats(D);
+            float *out = partial + (((size_t)kv * per_head / parts + row_block_id(g, C::ROWS, b.seq, p.q0, i)) * parts + part) * prompt_part_floats(C::ROWS, D);
             const int r = 32 * wave + 16 * s + n16;
 #pragma unroll
             for (int e = 0; e < DT; ++e) *reinterpret_cast<f32x4 *>(out + r * D + 16 * e + 4 * q4) = oacc[s][e];
@@ -330,7 +334,7 @@ __global__ __launch_bounds__(512) void prompt_attn_kernel(PromptGeom g, int per_
 }
 
 // The parts of a row put together, a wavefront for each (token, query head): lane l has D / 64 columns.
-template <int D>
+template <int D, int ROWS>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g, int per_kv, int parts, const float *__restrict__ partial,
                                                           uint16_t *__restrict__ O, float *__restrict__ lse)
 {
@@ -347,9 +351,9 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g, int per_
     }
     const PromptSeq p = prompt_seq(g, lo);
     if (tok < p.q0 || tok >= p.q0 + p.n) return;
-    const int r = (tok - p.q0) * g.G + (a - kv * g.G), i = r / PROMPT_ROWS, at = r - i * PROMPT_ROWS;
-    const float *from = partial + ((size_t)kv * per_kv + row_block_id(g, PROMPT_ROWS, lo, p.q0, i)) * parts * prompt_part_floats(D);
-    const float2 ml = lane < parts ? *reinterpret_cast<const float2 *>(from + lane * prompt_part_floats(D) + PROMPT_ROWS * D + 2 * at)
+    const int r = (tok - p.q0) * g.G + (a - kv * g.G), i = r / ROWS, at = r - i * ROWS;
+    const float *from = partial + ((size_t)kv * per_kv + row_block_id(g, ROWS, lo, p.q0, i)) * parts * prompt_part_floats(ROWS, D);
+    const float2 ml = lane < parts ? *reinterpret_cast<const float2 *>(from + lane * prompt_part_floats(ROWS, D) + ROWS * D + 2 * at)
                                    : make_float2(-INFINITY, 0.f);
     float M = ml.x;
 #pragma unroll
@@ -365,7 +369,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g, int per_
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int k = 0; k < N; ++k) y[u][k] = from[min(x + u, parts - 1) * prompt_part_floats(D) + at * D + N * lane + k];
+            for (int k = 0; k < N; ++k) y[u][k] = from[min(x + u, parts - 1) * prompt_part_floats(ROWS, D) + at * D + N * lane + k];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const float wx = x + u < parts ? __shfl(w, x + u, 64) : 0.f;
@@ -381,29 +385,30 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g, int per_
 
 // How many workgroups share a block's keys: as many as fill the chip's 256 CUs once, each with eight tiles at least (of all keys: where
 // a sequence has fewer than the batch, its parts are shorter).
+constexpr int SPLIT_WAVES = 8;
 static int prompt_parts(const PromptGeom &g)
 {
-    const long long blocks = g.Hkv * row_block_bound(g, PROMPT_ROWS), tiles = (g.Tk + KEY_TILE - 1) / KEY_TILE;
+    const long long blocks = g.Hkv * row_block_bound(g, 32 * SPLIT_WAVES), tiles = (g.Tk + KEY_TILE - 1) / KEY_TILE;
     return (int)std::max(1ll, std::min(std::min(256 / blocks, tiles / 8), 64ll));
 }
 
 static size_t prompt_partial_bytes(const PromptGeom &g, int D)
 {
     const int parts = prompt_parts(g);
-    return parts > 1 ? (size_t)g.Hkv * row_block_bound(g, PROMPT_ROWS) * parts * prompt_part_floats(D) * 4 : 0;
+    return parts > 1 ? (size_t)g.Hkv * row_block_bound(g, 32 * SPLIT_WAVES) * parts * prompt_part_floats(32 * SPLIT_WAVES, D) * 4 : 0;
 }
 size_t prompt_workspace_bytes(const PromptGeom &g, int D) { return prompt_partial_bytes(g, D); }
 
-template <int D, bool SPLIT>
+template <int D, int WAVES, bool SPLIT>
 static hipError_t launch_walk(const PromptGeom &g, int parts, const uint16_t *Q, const uint16_t *K, const uint16_t *V, uint16_t *O,
                               float *lse, float *partial, hipStream_t st)
 {
-    using C = Prompt<D>;
+    using C = Prompt<D, WAVES>;
     static LdsOptIn opted;  // one per kernel instantiation
-    const hipError_t e = opted.ensure(reinterpret_cast<const void *>(&prompt_attn_kernel<D, SPLIT>), C::BYTES);
+    const hipError_t e = opted.ensure(reinterpret_cast<const void *>(&prompt_attn_kernel<D, WAVES, SPLIT>), C::BYTES);
     if (e != hipSuccess) return e;
     const int per_head = (int)row_block_bound(g, C::ROWS) * parts;
-    hipLaunchKernelGGL((prompt_attn_kernel<D, SPLIT>), dim3(head_grid(g.Hkv, per_head)), dim3(C::THREADS), C::BYTES, st, g, per_head,
+    hipLaunchKernelGGL((prompt_attn_kernel<D, WAVES, SPLIT>), dim3(head_grid(g.Hkv, per_head)), dim3(C::THREADS), C::BYTES, st, g, per_head,
                        parts, Q, K, V, O, lse, partial);
     return hipGetLastError();
 }
@@ -413,11 +418,11 @@ static hipError_t launch_prompt_d(const PromptGeom &g, const uint16_t *Q, const 
                                   float *partial, hipStream_t st)
 {
     const int parts = prompt_parts(g);
-    if (parts == 1) return launch_walk<D, false>(g, 1, Q, K, V, O, lse, nullptr, st);
-    const hipError_t e = launch_walk<D, true>(g, parts, Q, K, V, O, lse, partial, st);
+    if (parts == 1) return getenv("W4") ? launch_walk<D, 4, false>(g, 1, Q, K, V, O, lse, nullptr, st) : launch_walk<D, 8, false>(g, 1, Q, K, V, O, lse, nullptr, st);
+    const hipError_t e = launch_walk<D, SPLIT_WAVES, true>(g, parts, Q, K, V, O, lse, partial, st);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((prompt_join_kernel<D>), dim3((unsigned)(((long long)g.Tq * g.Hq + 3) / 4)), dim3(256), 0, st, g,
-                       (int)row_block_bound(g, PROMPT_ROWS), parts, partial, O, lse);
+    hipLaunchKernelGGL((prompt_join_kernel<D, 32 * SPLIT_WAVES>), dim3((unsigned)(((long long)g.Tq * g.Hq + 3) / 4)), dim3(256), 0, st, g,
+                       (int)row_block_bound(g, 32 * SPLIT_WAVES), parts, partial, O, lse);
     return hipGetLastError();
 }
 

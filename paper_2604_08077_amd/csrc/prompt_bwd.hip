@@ -20,17 +20,18 @@
 
 namespace adaspark {
 
-constexpr int PB_THREADS = 512;
-constexpr int PB_BLOCK = 256;  // rows (dQ) or keys (dK, dV) of a workgroup: 8 wavefronts x 2 x 16
+constexpr int PB_WAVES = 4;
+constexpr int PB_THREADS = 64 * PB_WAVES;
+constexpr int PB_BLOCK = 32 * PB_WAVES;  // rows (dQ) or keys (dK, dV) of a workgroup
 
 template <int D>
 struct PromptBwd {
     static constexpr int TILE = 64 * D * 2;
     static constexpr int CPR = D / 8, RPI = 64 / CPR;
-    static constexpr int PER = 64 / RPI / 8;  // direct-to-LDS instructions per wavefront, tile and operand
+    static constexpr int PER = 64 / RPI / PB_WAVES;  // direct-to-LDS instructions per wavefront, tile and operand
     static constexpr int OFF_LSE = 2 * TILE;  // behind the two tiles (dK/dV kernel): 64 start values of S, 64 of dP
     static constexpr int STAGE = 2 * TILE + 512;
-    static constexpr int NST = 3;
+    static constexpr int NST = PB_WAVES == 8 ? 3 : 2;
     static constexpr int BYTES = NST * STAGE;
     static_assert(BYTES <= 160 * 1024, "LDS of one CU");
 };
@@ -42,7 +43,7 @@ struct PromptSpans {
     int most;          // spans of a block at most
 };
 constexpr int SPAN_MIN = 4;        // tiles; a span's sums are written and read again, about as much time as two take
-constexpr int SPAN_ITEMS = 768;    // workgroups that the tiles of all blocks are to be shared out to, three per CU
+constexpr int SPAN_ITEMS = 1536;   // workgroups that the tiles of all blocks are to be shared out to, six per CU
 static long long key_block_bound(const PromptGeom &g) { return (long long)g.Tk / PB_BLOCK + g.B; }
 __device__ __forceinline__ int key_block_id(int s, int k0, int j) { return k0 / PB_BLOCK + s + j; }
 
@@ -130,7 +131,7 @@ __global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most
 }
 
 template <int D>
-__global__ __launch_bounds__(PB_THREADS) void prompt_dq_kernel(PromptGeom g, int per_head, const uint16_t *__restrict__ Q,
+__global__ __launch_bounds__(PB_THREADS, 2) void prompt_dq_kernel(PromptGeom g, int per_head, const uint16_t *__restrict__ Q,
                                                                const uint16_t *__restrict__ K, const uint16_t *__restrict__ V,
                                                                const uint16_t *__restrict__ dO, const float *__restrict__ lse2p,
                                                                const float *__restrict__ deltap, uint16_t *__restrict__ dQ)
@@ -141,14 +142,13 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dq_kernel(PromptGeom g, int
     const int lane = threadIdx.x & 63, n16 = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-    int kv, slot, seq, blk;
+    int kv, slot;
     if (!head_slot(blockIdx.x, g.Hkv, per_head, kv, slot)) return;
-    if (!prompt_block(g, slot, (g.Tk + KEY_TILE - 1) / KEY_TILE,
-                      [&](int n, int m, int t) { return row_blocks<PB_BLOCK>(n, m, g.G, g.causal, t); }, seq, blk))
-        return;
-    seq = __builtin_amdgcn_readfirstlane(seq);
-    const PromptSeq p = prompt_seq(g, seq);
-    const int rows = p.n * g.G, row0 = ((rows - 1) / PB_BLOCK - blk) * PB_BLOCK;
+    const PromptBlock b = longest_first(g, slot, (g.Tk + KEY_TILE - 1) / KEY_TILE,
+                                        [&](int n, int m, int t) { return row_blocks<PB_BLOCK>(n, m, g.G, g.causal, t); });
+    if (b.seq < 0) return;
+    const PromptSeq p = b.p;
+    const int rows = p.n * g.G, row0 = ((rows - 1) / PB_BLOCK - b.block) * PB_BLOCK;
     auto reach_of = [&](int row) { return g.causal ? p.m - p.n + token_of_row(g, row) : p.m - 1; };
     auto tiles_to = [&](int row) {
         const int r = reach_of(min(row, rows - 1));
@@ -182,16 +182,28 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dq_kernel(PromptGeom g, int
 
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem);
     const uint16_t *khead = K + (size_t)p.k0 * g.ks + (size_t)kv * D, *vhead = V + (size_t)p.k0 * g.vs + (size_t)kv * D;
+    uint32_t kofs[C::PER], vofs[C::PER];
+#pragma unroll
+    for (int u = 0; u < C::PER; ++u) {
+        const int r = (wave * C::PER + u) * C::RPI + lane / C::CPR, chunk = (((lane & 15) ^ row_swizzle<D>(r)) & (C::CPR - 1)) * 8;
+        kofs[u] = (uint32_t)(r * (int)g.ks + chunk) * 2u;
+        vofs[u] = (uint32_t)(r * (int)g.vs + chunk) * 2u;
+    }
     // (keys past the sequence's last are that one again)
     auto issue = [&](int t, int stage) __attribute__((always_inline)) {
-        const int key = t * KEY_TILE, last = min(KEY_TILE - 1, p.m - 1 - key);
+        const int key = t * KEY_TILE, beyond = KEY_TILE - 1 - (p.m - 1 - key);
         const void *kt = uniform_ptr(khead + (size_t)key * g.ks), *vt = uniform_ptr(vhead + (size_t)key * g.vs);
 #pragma unroll
         for (int u = 0; u < C::PER; ++u) {
-            const int r = (wave * C::PER + u) * C::RPI + lane / C::CPR, chunk = (((lane & 15) ^ row_swizzle<D>(r)) & (C::CPR - 1)) * 8;
             const uint32_t piece = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)(stage * C::STAGE + (wave * C::PER + u) * 1024));
-            dma_1k_s(piece, kt, (uint32_t)(min(r, last) * (int)g.ks + chunk) * 2u);
-            dma_1k_s(piece + C::TILE, vt, (uint32_t)(min(r, last) * (int)g.vs + chunk) * 2u);
+            uint32_t ko = kofs[u], vo = vofs[u];
+            if (beyond > 0) {
+                const int r = (wave * C::PER + u) * C::RPI + lane / C::CPR, over = max(0, r - (KEY_TILE - 1 - beyond));
+                ko -= (uint32_t)(over * (int)g.ks) * 2u;
+                vo -= (uint32_t)(over * (int)g.vs) * 2u;
+            }
+            dma_1k_s(piece, kt, ko);
+            dma_1k_s(piece + C::TILE, vt, vo);
         }
     };
 
@@ -266,12 +278,10 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dq_kernel(PromptGeom g, int
     static_assert(KSTEPS % 2 == 0 && DT % 2 == 0, "the operands' two places take turns");
 
     if (ntiles > 0) issue(0, 0);
-    if (ntiles > 1) issue(1, 1);
-    for (int t = 0, stage = 0; t < ntiles; ++t, stage = stage == 2 ? 0 : stage + 1) {
-        if (t + 1 < ntiles) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * C::PER) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (t + 2 < ntiles) issue(t + 2, stage == 0 ? 2 : stage - 1);  // (the stage read last at tile t - 1)
-        if (t < mine) work(t, stage);
+    for (int t = 0; t < ntiles; ++t) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t + 1 < ntiles) issue(t + 1, (t + 1) & 1);  // (the stage read last at tile t - 1)
+        if (t < mine) work(t, t & 1);
     }
     const float c = 1.0f / sqrtf((float)D);
 #pragma unroll
@@ -284,19 +294,19 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dq_kernel(PromptGeom g, int
 }
 
 // Key blocks of a sequence whose walk over the rows has at least t tiles of 64; the first blocks walk farthest.
-__device__ __forceinline__ int key_blocks(int n, int m, int G, int causal, int t)
+__device__ __forceinline__ int key_blocks(const PromptGeom &g, int n, int m, int t)
 {
     const int nb = (m + PB_BLOCK - 1) / PB_BLOCK;
     if (t == 0) return nb;
-    const long long rows = (long long)n * G - 64ll * (t - 1);  // a block has such a walk if its first row lies before this one
+    const long long rows = (long long)n * g.G - 64ll * (t - 1);  // a block has such a walk if its first row lies before this one
     if (rows <= 0) return 0;
-    if (!causal) return nb;
-    const long long key = (rows - 1) / G + (m - n);  // the last key whose first row does
-    return key < 0 ? 0 : (int)min((long long)nb, key / PB_BLOCK + 1);
+    if (!g.causal) return nb;
+    const int key = token_of_row(g, (int)(rows - 1)) + (m - n);  // the last key whose first row does
+    return key < 0 ? 0 : min(nb, key / PB_BLOCK + 1);
 }
 
 template <int D>
-__global__ __launch_bounds__(PB_THREADS) void prompt_dkv_kernel(PromptGeom g, int per_head, PromptSpans cut,
+__global__ __launch_bounds__(PB_THREADS, 2) void prompt_dkv_kernel(PromptGeom g, int per_head, PromptSpans cut,
                                                                 const int *__restrict__ span_p, const uint16_t *__restrict__ Q, const uint16_t *__restrict__ K,
                                                                 const uint16_t *__restrict__ V, const uint16_t *__restrict__ dO,
                                                                 const float *__restrict__ lse2p, const float *__restrict__ deltap,
@@ -304,20 +314,19 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dkv_kernel(PromptGeom g, in
                                                                 uint16_t *__restrict__ dV)
 {
     using C = PromptBwd<D>;
-    constexpr int NS = 2, KSTEPS = D / 32, DT = D / 16, PER = C::PER;
+    constexpr int NS = 2, KSTEPS = D / 32, DT = D / 16, PER = C::PER, CPR = C::CPR;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const int lane = threadIdx.x & 63, n16 = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-    int kv, slot, seq, j;
+    int kv, slot;
     if (!head_slot(blockIdx.x, g.Hkv, per_head, kv, slot)) return;
     const int span = slot % cut.most, span_len = *span_p;
-    if (!prompt_block(g, slot / cut.most, (int)(((long long)g.Tq * g.G + 63) / 64),
-                      [&](int n, int m, int t) { return key_blocks(n, m, g.G, g.causal, t); }, seq, j))
-        return;
-    seq = __builtin_amdgcn_readfirstlane(seq);
-    j = __builtin_amdgcn_readfirstlane(j);
-    const PromptSeq p = prompt_seq(g, seq);
+    const PromptBlock b = longest_first(g, slot / cut.most, (int)(((long long)g.Tq * g.G + 63) / 64),
+                                        [&](int n, int m, int t) { return key_blocks(g, n, m, t); });
+    if (b.seq < 0) return;
+    const PromptSeq p = b.p;
+    const int j = b.block;
     const int rows = p.n * g.G, off = p.m - p.n;
     auto first_row = [&](int key) { return g.causal ? (int)min((long long)rows, max(0ll, (long long)key - off) * g.G) : 0; };  // that attends it
     const int first = first_row(j * PB_BLOCK);
@@ -353,23 +362,45 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dkv_kernel(PromptGeom g, in
         asm volatile("" : "+v"(l));
         return l;
     };
-    // Tile t of the span.  Rows past the sequence's last are that one again, under start values that give them no part.
+    // Tile t of the span.  With the tile's first row the ph-th of token t0's, the tile's row r is x = ph + r rows behind that token's
+    // first one: x / G tokens on, and as many times `skip` further than x rows in a row.  Piece u of this wavefront is RPI rows, a
+    // 16-byte slot to a lane; its place in the tile is that of piece 0 with some bits flipped (row_swizzle's, and u KB): six vector instructions
+    // a piece, all else is the wavefront's.  Rows past the sequence's last are that one again, under start values that give them no part.
+    const int qskip = (int)(g.qs - (long long)g.G * D) * 2, oskip = (g.Hq - g.G) * D * 2;  // bytes from a token's last row to the next one's first
     auto issue = [&](int t, int stage) __attribute__((always_inline)) {
-        const uint32_t dst = lds0 + (uint32_t)(stage * C::STAGE);
-        const int l = fresh_lane(), r0 = row0 + 64 * t;
+        const int l = fresh_lane(), r0 = row0 + 64 * t, t0 = __builtin_amdgcn_readfirstlane(token_of_row(g, r0)), ph = r0 - t0 * g.G;
+        const uint32_t dst = lds0 + (uint32_t)(stage * C::STAGE), piece0 = __builtin_amdgcn_readfirstlane(dst + (uint32_t)(wave * PER * 1024));
+        const uint32_t vals = __builtin_amdgcn_readfirstlane(dst + C::OFF_LSE + 256 * wave);
+        const float *start = (wave == 0 ? lse2p : deltap);
+        const size_t token = (size_t)(p.q0 + t0);
+        const int w0 = ph + wave * PER * C::RPI, most = rows - 1 - t0 * g.G;
+        const int j = l / CPR, slot0 = j * (D * 2) + (((l & 15) ^ row_swizzle<D>(j)) & (CPR - 1)) * 16;
+        if (r0 + 64 <= rows) {
+            const void *qt = uniform_ptr(Q + token * g.qs + (size_t)(kv * g.G + w0) * D), *ot = uniform_ptr(dO + (token * g.Hq + kv * g.G + w0) * D);
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int r = (wave * PER + u) * C::RPI + l / C::CPR;
-            const int row = min(r0 + r, rows - 1), tok = token_of_row(g, row), head = kv * g.G + (row - tok * g.G);
-            const int chunk = (((l & 15) ^ row_swizzle<D>(r)) & (C::CPR - 1)) * 8;
-            const uint32_t piece = __builtin_amdgcn_readfirstlane(dst + (uint32_t)((wave * PER + u) * 1024));
-            dma_lane16(piece, Q + (size_t)(p.q0 + tok) * g.qs + head * D + chunk);
-            dma_lane16(piece + C::TILE, dO + ((size_t)(p.q0 + tok) * g.Hq + head) * D + chunk);
-        }
-        if (wave < 2) {  // the start values: wavefront 0 of S, wavefront 1 of dP
-            const int row = r0 + l, tok = token_of_row(g, row);
-            const size_t at = row < rows ? (size_t)(p.q0 + tok) * g.Hq + kv * g.G + (row - tok * g.G) : (size_t)g.Tq * g.Hq;
-            dma_lane4(__builtin_amdgcn_readfirstlane(dst + C::OFF_LSE + 256 * wave), (wave == 0 ? lse2p : deltap) + at);
+            for (int u = 0; u < PER; ++u) {
+                const uint32_t tok = token_of_near_row(g, (uint32_t)(w0 + u * C::RPI + j));
+                const uint32_t at = (uint32_t)slot0 ^ (uint32_t)(u * 1024 + ((row_swizzle<D>(u * C::RPI) & (CPR - 1)) << 4));
+                dma_1k_s(piece0 + (uint32_t)(u * 1024), qt, at + __umul24(tok, (uint32_t)qskip));
+                dma_1k_s(piece0 + (uint32_t)(u * 1024 + C::TILE), ot, at + __umul24(tok, (uint32_t)oskip));
+            }
+            if (wave < 2) {  // the start values: wavefront 0 of S, wavefront 1 of dP
+                const uint32_t x = (uint32_t)(ph + l);
+                dma_256_s(vals, uniform_ptr(start + token * g.Hq + kv * g.G), 4u * (x + __umul24(token_of_near_row(g, x), (uint32_t)(g.Hq - g.G))));
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+                const int r = (wave * PER + u) * C::RPI + j, x = min(ph + r, most), tok = (int)token_of_near_row(g, (uint32_t)x);
+                const size_t head = kv * g.G + (x - tok * g.G);
+                const int chunk = (((l & 15) ^ row_swizzle<D>(r)) & (CPR - 1)) * 8;
+                dma_lane16(piece0 + (uint32_t)(u * 1024), Q + (token + tok) * g.qs + head * D + chunk);
+                dma_lane16(piece0 + (uint32_t)(u * 1024 + C::TILE), dO + ((token + tok) * g.Hq + head) * D + chunk);
+            }
+            if (wave < 2) {
+                const int x = ph + l, tok = (int)token_of_near_row(g, (uint32_t)x);
+                dma_lane4(vals, start + (x <= most ? (token + tok) * g.Hq + kv * g.G + (x - tok * g.G) : (size_t)g.Tq * g.Hq));
+            }
         }
     };
     const uint32_t nat0 = (uint32_t)row_tile_off<D>(n16, q4);
@@ -420,7 +451,7 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dkv_kernel(PromptGeom g, in
                     const int row = r0 + 16 * (2 * H + x) + 4 * q4;
 #pragma unroll
                     for (int s = 0; s < NS; ++s) {
-                        const int from = first_row(key0 + 16 * s + n16);
+                        const int from = g.causal ? min(max(key0 + 16 * s + n16 - off, 0), p.n) * g.G : 0;
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
                             if (row + v < from) sa[s][v] = -INFINITY;
@@ -452,25 +483,20 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dkv_kernel(PromptGeom g, in
     };
 
     if (ntiles > 0) issue(0, 0);
-    if (ntiles > 1) issue(1, 1);
-    int t = 0, stage = 0;
+    int t = 0;
     auto tile = [&](auto edge_tag) __attribute__((always_inline)) {
-        // this wavefront's loads of the tile have landed (those of the next may stay in flight), then everybody's
-        if (t + 1 >= ntiles) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        else if (wave < 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * PER + 1) : "memory");
-        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * PER) : "memory");
-        if (t + 2 < ntiles) issue(t + 2, stage == 0 ? 2 : stage - 1);  // (the stage read last at tile t - 1)
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // everybody's loads of the tile have landed
+        if (t + 1 < ntiles) issue(t + 1, (t + 1) & 1);  // (the stage read last at tile t - 1)
         const int r0 = row0 + 64 * t;
-        if (busy && (!decltype(edge_tag)::value || r0 + 63 >= mine_from)) work(stage, r0, edge_tag);
+        if (busy && (!decltype(edge_tag)::value || r0 + 63 >= mine_from)) work(t & 1, r0, edge_tag);
         ++t;
-        stage = stage == 2 ? 0 : stage + 1;
     };
     while (t < ntiles && row0 + 64 * t < mine_all) tile(std::true_type{});
     while (t < ntiles) tile(std::false_type{});
 
     if (spans > 1) {
         f32x4 *sums = reinterpret_cast<f32x4 *>(partial) +
-                      (((size_t)kv * cut.blocks + key_block_id(seq, p.k0, j)) * cut.most + span) * (2 * PB_BLOCK * D / 4) + wave * (NS * DT * 64) + lane;
+                      (((size_t)kv * cut.blocks + key_block_id(b.seq, p.k0, j)) * cut.most + span) * (2 * PB_BLOCK * D / 4) + wave * (NS * DT * 64) + lane;
 #pragma unroll
         for (int x = 0; x < NS * DT; ++x) {
             sums[x * 64] = accV[x / DT][x % DT];
@@ -492,14 +518,14 @@ __global__ __launch_bounds__(PB_THREADS) void prompt_dkv_kernel(PromptGeom g, in
     }
 }
 
-// The spans' sums of a key block, added in their order: eight workgroups to a block, one for each wavefront's keys; NS * DT * 64
+// The spans' sums of a key block, added in their order: four workgroups to a block, one for each wavefront's keys; NS * DT * 64
 // places in MFMA output order.
 template <int D>
 __global__ __launch_bounds__(256) void prompt_reduce_kernel(PromptGeom g, PromptSpans cut, const int *__restrict__ span_p, const float *__restrict__ partial,
                                                             uint16_t *__restrict__ dK, uint16_t *__restrict__ dV)
 {
     constexpr int NS = 2, DT = D / 16;
-    const int wave = blockIdx.x & 7, kv = (int)((blockIdx.x >> 3) % (unsigned)g.Hkv), id = (int)((blockIdx.x >> 3) / (unsigned)g.Hkv);
+    const int wave = blockIdx.x % PB_WAVES, kv = (int)(blockIdx.x / PB_WAVES % (unsigned)g.Hkv), id = (int)(blockIdx.x / PB_WAVES / (unsigned)g.Hkv);
     int lo = 0, hi = g.B;  // the sequence of block `id`: the last one whose blocks begin at or before it
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -548,7 +574,7 @@ static hipError_t launch_bwd(const PromptGeom &g, const uint16_t *Q, const uint1
         hipLaunchKernelGGL((prompt_dkv_kernel<D>), dim3(head_grid(g.Hkv, keys)), dim3(PB_THREADS), C::BYTES, st, g, keys, cut, w.span, Q, K, V, dO,
                            w.lse2, w.delta, w.part, dK, dV);
         if (cut.most > 1)
-            hipLaunchKernelGGL((prompt_reduce_kernel<D>), dim3((unsigned)(cut.blocks * g.Hkv * 8)), dim3(256), 0, st, g, cut, w.span, w.part, dK, dV);
+            hipLaunchKernelGGL((prompt_reduce_kernel<D>), dim3((unsigned)(cut.blocks * g.Hkv * PB_WAVES)), dim3(256), 0, st, g, cut, w.span, w.part, dK, dV);
     }
     if (g.Tq > 0) {
         const int blocks = (int)row_block_bound(g, PB_BLOCK);

@@ -33,7 +33,8 @@ BAD_PROMPTS = BAD_HEADS + [
     (dict(sequences=0), EINVAL), (dict(q_tokens=-1), EINVAL), (dict(k_tokens=-1), EINVAL),
     (dict(q_stride=255), EINVAL), (dict(q_stride=260), EINVAL), (dict(k_stride=64), EINVAL), (dict(v_stride=-8), EINVAL),
     (dict(v_stride=(1 << 22) + 8), EUNSUPPORTED), (dict(q_tokens=1 << 30), EUNSUPPORTED), (dict(k_tokens=(1 << 30)), EUNSUPPORTED),
-    (dict(sequences=1 << 24), EUNSUPPORTED)]
+    (dict(sequences=1 << 24), EUNSUPPORTED),
+    (dict(q_heads=258), EUNSUPPORTED)]
 BAD_CACHES = BAD_HEADS + [
     (dict(sequences=0), EINVAL), (dict(pages=0), EINVAL), (dict(page_size=0), EINVAL), (dict(table_pages=0), EINVAL),
     (dict(format=2), EINVAL), (dict(page_size=24), EUNSUPPORTED), (dict(page_size=1 << 20, table_pages=1 << 11), EUNSUPPORTED),
