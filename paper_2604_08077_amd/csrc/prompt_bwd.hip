@@ -42,8 +42,8 @@ struct PromptSpans {
     long long blocks;  // bound of the key blocks per KV head
     int most;          // spans of a block at most
 };
-constexpr int SPAN_MIN = 4;        // tiles; a span's sums are written and read again, about as much time as two take
-constexpr int SPAN_ITEMS = 1536;   // workgroups that the tiles of all blocks are to be shared out to, six per CU
+constexpr int SPAN_MIN = 8;        // tiles; a span's sums are written and read again, about as much time as two take
+constexpr int SPAN_ITEMS = 1024;   // workgroups that the tiles of all blocks are to be shared out to, four per CU
 static long long key_block_bound(const PromptGeom &g) { return (long long)g.Tk / PB_BLOCK + g.B; }
 __device__ __forceinline__ int key_block_id(int s, int k0, int j) { return k0 / PB_BLOCK + s + j; }
 
@@ -321,8 +321,10 @@ __global__ __launch_bounds__(PB_THREADS, 2) void prompt_dkv_kernel(PromptGeom g,
 
     int kv, slot;
     if (!head_slot(blockIdx.x, g.Hkv, per_head, kv, slot)) return;
-    const int span = slot % cut.most, span_len = *span_p;
-    const PromptBlock b = longest_first(g, slot / cut.most, (int)(((long long)g.Tq * g.G + 63) / 64),
+    // Later spans first (only long blocks have them), and the first span of all blocks last: the launch ends with its shortest items.  And
+    // an XCD gets every so many-th block, not every so many-th span.
+    const int nb = (int)cut.blocks, span = cut.most - 1 - slot / nb, span_len = *span_p;
+    const PromptBlock b = longest_first(g, slot % nb, (int)(((long long)g.Tq * g.G + 63) / 64),
                                         [&](int n, int m, int t) { return key_blocks(g, n, m, t); });
     if (b.seq < 0) return;
     const PromptSeq p = b.p;
@@ -330,9 +332,10 @@ __global__ __launch_bounds__(PB_THREADS, 2) void prompt_dkv_kernel(PromptGeom g,
     const int rows = p.n * g.G, off = p.m - p.n;
     auto first_row = [&](int key) { return g.causal ? (int)min((long long)rows, max(0ll, (long long)key - off) * g.G) : 0; };  // that attends it
     const int first = first_row(j * PB_BLOCK);
-    const int all = (rows - first + 63) / 64, spans = max(1, (all + span_len - 1) / span_len);
+    // (a block's spans are equally long)
+    const int all = (rows - first + 63) / 64, spans = max(1, (all + span_len - 1) / span_len), len = (all + spans - 1) / spans;
     if (span >= spans) return;
-    const int row0 = first + span * span_len * 64, ntiles = min(span_len, all - span * span_len);
+    const int row0 = first + span * len * 64, ntiles = max(0, min(len, all - span * len));
 
     const int key0 = j * PB_BLOCK + wave * 32;
     const bool busy = key0 < p.m;
