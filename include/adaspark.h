@@ -401,7 +401,9 @@ int adaspark_prompt_attn(const adaspark_prompts *prompts, const void *Q, const v
 /*
  * Its backward pass, with delta = dO.O per row:
  *   dV_j = sum p_j dO,  dS_j = p_j (dO.v_j - delta),  dQ = sum_j dS_j k_j / sqrt(head_dim),  dK_j = sum dS_j q / sqrt(head_dim)
- * (dK, dV summed over all rows and all query heads of the KV head's group).
+ * (dK, dV summed over all rows and all query heads of the KV head's group).  sum_j dS_j is 0 in a row but for what the rounding of
+ * O leaves in delta; dQ is taken as sum_j dS_j (k_j - r) / sqrt(head_dim) with r the mean of up to 64 keys of the sequence, which keeps that
+ * remainder out of a direction that all keys share.
  *   O, lse     in   as adaspark_prompt_attn returned them;  dO  in  bf16 [q_tokens][q_heads][head_dim], contiguous
  *   dQ         out  bf16 [q_tokens][q_heads][head_dim];  dK, dV  out  bf16 [k_tokens][kv_heads][head_dim], contiguous
  *   workspace       adaspark_prompt_workspace_bytes(ADASPARK_PROMPT_ATTN_BWD)

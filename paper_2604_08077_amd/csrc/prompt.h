@@ -196,6 +196,119 @@ __device__ __forceinline__ int row_block_id(const PromptGeom &g, int R, int s, i
     return (int)((long long)q0 * g.G / R) + s + i;
 }
 
+// Few blocks (a short turn on a long history, a handful of prompts): each block's walk over the keys is shared out to several
+// workgroups, a part each, and a second kernel puts a row's parts together.  A workgroup's item is (block, part); the parts of a block are
+// equally long, at most `chunk` tiles, and chunk follows from the lengths: as short as the number of items, `cap` a KV head, allows.
+constexpr int PART_MIN = 8;      // tiles: a part's result is written and read again, and a second launch made
+constexpr int PARTS_MAX = 64;    // of a block
+constexpr int PART_BLOCKS = 768; // blocks up to which walks are shared out: three to a place for a workgroup, 512 of which 256 CUs have
+struct PromptCut {
+    int cap;           // items of a KV head at most; 0: walks are not shared out
+    long long blocks;  // blocks of a KV head at most
+};
+inline PromptCut prompt_cut(const PromptGeom &g, int R)
+{
+    PromptCut c = {0, row_block_bound(g, R)};
+    const long long blocks = c.blocks * g.Hkv;
+    if (g.B > PROMPT_SEQS || blocks > PART_BLOCKS || (g.Tk + KEY_TILE - 1) / KEY_TILE <= PART_MIN) return c;
+    c.cap = (int)((2 * blocks > 512 ? 2 * blocks : 512) / g.Hkv);
+    return c;
+}
+// What the second kernel goes by, in the workspace: for every block the number of its parts, and each part's item, whose number is
+// that of its place among the parts' results.
+struct PromptParts {
+    int *count, *item;  // [Hkv][blocks], [Hkv][blocks][PARTS_MAX]
+    float *result;      // [Hkv][cap][floats]
+    size_t bytes;
+};
+inline PromptParts prompt_parts(const PromptGeom &g, const PromptCut &c, size_t floats, void *ws)
+{
+    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    PromptParts p = {nullptr, nullptr, nullptr, 0};
+    if (c.cap == 0) return p;
+    unsigned char *at = static_cast<unsigned char *>(ws);
+    const size_t blocks = (size_t)g.Hkv * c.blocks, a = up(blocks * 4), b = up(blocks * PARTS_MAX * 4);
+    p.count = reinterpret_cast<int *>(at);
+    p.item = reinterpret_cast<int *>(at + a);
+    p.result = reinterpret_cast<float *>(at + a + b);
+    p.bytes = a + b + (size_t)g.Hkv * c.cap * floats * 4;
+    return p;
+}
+
+// Item w of a KV head: its block, which of the block's parts, and `chunk`.  Items come by parts: all blocks' first ones, then the second ones
+// of the blocks that have one, ...  seq -1: there is no such item.
+//
+// A block has max(1, ceil(walk / chunk)) parts, so there are at most blocks + tiles / chunk items, with `tiles` those of all walks.  A
+// bound of it: row block i of a sequence reaches to m - n + min(n, R (i + 1) / G + 1) keys or less, and ceil(x / 64) < x / 64 + 1.
+struct PromptItem {
+    PromptBlock b;
+    int part, chunk;
+};
+template <int R>
+__device__ __forceinline__ PromptItem prompt_item(const PromptGeom &g, int w, int cap)
+{
+    auto count = [&](int n, int m, int t) { return row_blocks<R>(n, m, g.G, g.causal, t); };
+    const PromptLengths l = prompt_lengths(g, 0);
+    float tiles = 0.f;
+    int longest = 0;
+#pragma unroll
+    for (int c = 0; c < PROMPT_CHUNKS; ++c)
+        if (c < l.chunks) {
+            const float n = (float)l.n[c], m = (float)l.m[c], nb = (float)count(l.n[c], l.m[c], 0);
+            const float keys = g.causal ? fminf(nb * m, nb * fmaxf(m - n, 0.f) + fminf(nb * n, nb + (float)R / (float)g.G * 0.5f * nb * (nb + 1.f))) : nb * m;
+            tiles += nb + keys * (1.f / KEY_TILE);
+            longest = max(longest, l.m[c]);
+        }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        tiles += __shfl_xor(tiles, d, 64);
+        longest = max(longest, __shfl_xor(longest, d, 64));
+    }
+    PromptItem it = {{{0, 0, 0, 0}, -1, 0}, 0, 0};
+    int blocks = blocks_from(l, 0, count);
+    const int share = (int)(tiles * 1.0001f / (float)max(1, cap - blocks)) + 1;  // (the sums above are off by less)
+    it.chunk = __builtin_amdgcn_readfirstlane(max(max(PART_MIN, share), (longest / KEY_TILE + PARTS_MAX) / PARTS_MAX));
+    while (w >= blocks) {
+        if (blocks == 0 || it.part == PARTS_MAX - 1) return it;
+        w -= blocks;
+        ++it.part;
+        blocks = blocks_from(l, it.part * it.chunk + 1, count);
+    }
+    it.b = nth_block(l, w, it.part == 0 ? 0 : it.part * it.chunk + 1, -1, count);
+    return it;
+}
+
+// Row (token, query head) number `row` of Q, for a wavefront of the second kernel: its KV head, its place in its block, the block's parts;
+// lane i has the i-th part's item.  false: no sequence's, or a row whose one part wrote it.
+struct PartRow {
+    long long row;
+    int seq, kv, at, n, item;
+};
+__device__ __forceinline__ bool part_row(const PromptGeom &g, const PromptCut &cut, const PromptParts &parts, int R, long long row, PartRow &r)
+{
+    if (row >= (long long)g.Tq * g.Hq) return false;
+    const int tok = (int)(row / g.Hq), a = (int)(row - (long long)tok * g.Hq);
+    r.row = row;
+    r.kv = a / g.G;
+    int lo = 0, hi = g.B;  // the last sequence with a start at or before the token
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (g.q_start[mid] <= tok) lo = mid;
+        else hi = mid;
+    }
+    r.seq = lo;
+    const PromptSeq p = prompt_seq(g, lo);
+    if (tok < p.q0 || tok >= p.q0 + p.n) return false;
+    const int x = (tok - p.q0) * g.G + (a - r.kv * g.G), i = x / R;
+    r.at = x - i * R;
+    const size_t id = (size_t)r.kv * cut.blocks + row_block_id(g, R, lo, p.q0, i);
+    const int lane = threadIdx.x & 63, item = parts.item[id * PARTS_MAX + lane];
+    r.n = min(parts.count[id], PARTS_MAX);
+    if (r.n <= 1) return false;
+    r.item = lane < r.n ? min(max(item, 0), cut.cap - 1) : 0;  // (starts that overlap leave blocks that nobody worked)
+    return true;
+}
+
 size_t prompt_workspace_bytes(const PromptGeom &g, int D);
 hipError_t launch_prompt_attn(const PromptGeom &g, int D, const uint16_t *Q, const uint16_t *K, const uint16_t *V, uint16_t *O,
                               float *lse, void *ws, hipStream_t st);

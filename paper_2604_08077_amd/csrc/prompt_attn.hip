@@ -1,12 +1,17 @@
 // Attention over packed prompts (prompt.h): o = sum_j p_j v_j, p = softmax(c q.k_j), and the log-sum-exp, in one pass over the keys
 // with a running reference and sum per row.
 //
-// A workgroup takes 256 rows of one sequence and KV head -- with G query heads to a KV head the rows of 256 / G tokens, so that G heads share
+// A workgroup takes 128 rows of one sequence and KV head -- with G query heads to a KV head the rows of 128 / G tokens, so that G heads share
 // each key tile and all rows of a block reach about equally far -- and walks the keys in tiles of 64.  K and V go from the caller's
-// tensors straight into LDS, three stages each, rows as they are: S^T = K.Q^T reads a tile's rows, O^T += V^T.P^T reads it transposed
-// (ds_read_b64_tr_b16), and no packed copy is made first.  The eight wavefronts work in two sets in counter-phase, as the masked walk's
-// do (attn_walk.hip): a SIMD's two wavefronts take turns at the matrix pipes, one's softmax under the other's products.
-// A wavefront stops at the last tile that its own 32 rows reach.
+// tensors straight into LDS, two stages each, rows as they are: S^T = K.Q^T reads a tile's rows, O^T += V^T.P^T reads it transposed
+// (ds_read_b64_tr_b16), and no packed copy is made first.  Four wavefronts of 32 rows; a wavefront stops at the last tile that
+// its own rows reach.
+//
+// Bound by the matrix pipes and, at head-dim 64, by the exponentials and what surrounds them (an exponential, a multiply-add, an addition
+// and half a conversion for each score).  Two workgroups on a CU (three at head-dim 64) are not in step, so one's softmax, barriers and
+// first loads run under the other's products.  A workgroup of eight wavefronts with 256 rows and three stages, its two halves in counter-phase as in
+// attn_walk.hip, is as fast at head-dim 128 on long walks (32,768 tokens of 28/4 heads 6.0 ms either way) and slower on short ones (16 prompts of
+// 17 to 1,504 tokens 87 us, so 82) and at head-dim 64 (32,768 tokens of 8/2 heads 1.32 ms, 1.07; 4,096 85 us, 59).
 //
 // Score products are exact (bf16 x bf16 accumulated in fp32); the softmax scale is applied in fp32 with the reference, one
 // instruction.  Weights are rounded to bf16 for P.V only: the sum is of the fp32 weights, so the log-sum-exp carries no bf16 rounding.
@@ -19,12 +24,13 @@
 
 namespace adaspark {
 
-template <int D, int WAVES>
+template <int D>
 struct Prompt {
+    static constexpr int WAVES = 4;
     static constexpr int THREADS = 64 * WAVES;
     static constexpr int NS = 2;
     static constexpr int ROWS = 16 * NS * WAVES;
-    static constexpr int NST = WAVES == 8 ? 3 : 2;  // LDS stages of K and of V
+    static constexpr int NST = 2;  // LDS stages of K and of V
     static constexpr int PF = 4;   // operand loads in flight ahead of the MFMAs
     static constexpr int TILE = KEY_TILE * D * 2;
     static constexpr int CPR = D / 8;              // 16-byte chunks of a row
@@ -36,46 +42,49 @@ struct Prompt {
 };
 constexpr float LN2 = 0.69314718055994530942f;
 
+constexpr int PROMPT_ROWS = Prompt<64>::ROWS;
+
 // A part's result: O unnormalised, fp32 [rows][D], then (m, l) of each row (m in base 2).
-__host__ __device__ inline size_t prompt_part_floats(int rows, int D) { return (size_t)rows * (D + 2); }
+__host__ __device__ inline size_t prompt_part_floats(int D) { return (size_t)PROMPT_ROWS * (D + 2); }
 
-template <int KEEP>
-__device__ __forceinline__ void stage_barrier()
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptGeom g, PromptCut cut, PromptParts parts,
+                                                             const uint16_t *__restrict__ Q, const uint16_t *__restrict__ K,
+                                                             const uint16_t *__restrict__ V, uint16_t *__restrict__ O,
+                                                             float *__restrict__ lse)
 {
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(KEEP) : "memory");
-}
-
-template <int D, int WAVES, bool SPLIT>
-__global__ __launch_bounds__(64 * WAVES, 2) void prompt_attn_kernel(PromptGeom g, int per_head, int parts, const uint16_t *__restrict__ Q,
-                                                          const uint16_t *__restrict__ K, const uint16_t *__restrict__ V,
-                                                          uint16_t *__restrict__ O, float *__restrict__ lse,
-                                                          float *__restrict__ partial)
-{
-    using C = Prompt<D, WAVES>;
+    using C = Prompt<D>;
     constexpr int NS = C::NS, KSTEPS = D / 32, DT = D / 16, PF = C::PF;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
 
     const int lane = threadIdx.x & 63, n16 = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bool set_y = WAVES == 8 && wave >= 4;
 
     int kv, slot;
-    if (!head_slot(blockIdx.x, g.Hkv, per_head, kv, slot)) return;
-    const int part = SPLIT ? slot % parts : 0;
-    const PromptBlock b = longest_first(g, SPLIT ? slot / parts : slot, (g.Tk + KEY_TILE - 1) / KEY_TILE,
-                                        [&](int n, int m, int t) { return row_blocks<C::ROWS>(n, m, g.G, g.causal, t); });
-    if (b.seq < 0) return;
-    const PromptSeq p = b.p;
-    const int rows = p.n * g.G, i = (rows - 1) / C::ROWS - b.block, row0 = i * C::ROWS;
+    if (!head_slot(blockIdx.x, g.Hkv, SPLIT ? cut.cap : (int)cut.blocks, kv, slot)) return;
+    PromptItem it;
+    if constexpr (SPLIT) it = prompt_item<C::ROWS>(g, slot, cut.cap);
+    else it = {longest_first(g, slot, (g.Tk + KEY_TILE - 1) / KEY_TILE,
+                             [&](int n, int m, int t) { return row_blocks<C::ROWS>(n, m, g.G, g.causal, t); }), 0, 0};
+    if (it.b.seq < 0) return;
+    const PromptSeq p = it.b.p;
+    const int rows = p.n * g.G, i = (rows - 1) / C::ROWS - it.b.block, row0 = i * C::ROWS;
     auto reach_of = [&](int row) { return g.causal ? p.m - p.n + token_of_row(g, row) : p.m - 1; };  // the last key that a row attends
     auto tiles_to = [&](int row) { return max(0, reach_of(min(row, rows - 1)) / KEY_TILE + (reach_of(min(row, rows - 1)) >= 0 ? 1 : 0)); };
 
     // the tiles of the block's walk, and of the wavefront's: first .. first + count
     int first = 0, ntiles = __builtin_amdgcn_readfirstlane(tiles_to(row0 + C::ROWS - 1));
     int mine = row0 + 32 * wave < rows ? __builtin_amdgcn_readfirstlane(tiles_to(row0 + 32 * wave + 31)) : 0;
+    bool whole = true;  // the walk is all of the block's
     if (SPLIT) {
-        const int per = (ntiles + parts - 1) / parts;
-        first = min(part * per, ntiles);
+        const int n = max(1, (ntiles + it.chunk - 1) / it.chunk), per = (ntiles + n - 1) / n;
+        whole = n == 1;
+        if (threadIdx.x == 0) {
+            const size_t id = (size_t)kv * cut.blocks + row_block_id(g, C::ROWS, it.b.seq, p.q0, i);
+            if (it.part == 0) parts.count[id] = n;
+            parts.item[id * PARTS_MAX + it.part] = slot;
+        }
+        first = min(it.part * per, ntiles);
         ntiles = min(per, ntiles - first);
         mine = min(max(mine - first, 0), ntiles);
     }
@@ -143,25 +152,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void prompt_attn_kernel(PromptGeom g
         for (int e = 0; e < DT; ++e) oacc[s][e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // Slot t works on K(t) and V(t-1).  Three stages: K(t+1) and V(t) may be in flight when it opens, K(t+2) and V(t+1) are started into
-    // the stages that fell free (as in attn_walk.hip).  Two: K(t+1) and V(t) are started when it opens, and waited for at the next.
-    int kst = 0;  // stage of K(t); V(t-1) sits in the one before
-    auto before = [](int st) { return st == 0 ? C::NST - 1 : st - 1; };
-    auto after = [](int st) { return st == C::NST - 1 ? 0 : st + 1; };
+    // Slot t works on K(t) and V(t-1); K(t+1) and V(t) are started when it opens, and waited for at the next.
+    int kst = 0;  // stage of K(t); V(t-1) sits in the other
     auto open_slot = [&](int t) __attribute__((always_inline)) {
-        if (C::NST == 3) {
-            if (t > 0 && t + 1 < ntiles) stage_barrier<2 * C::DMA>();
-            else stage_barrier<0>();
-            if (t + 1 < ntiles) issue_v(t + 1, after(kst));
-            if (t + 2 < ntiles) issue_k(t + 2, before(kst));
-        } else {
-            stage_barrier<0>();
-            if (t > 0 && t < ntiles) issue_v(t, kst);
-            if (t + 1 < ntiles) issue_k(t + 1, after(kst));
-        }
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t > 0 && t < ntiles) issue_v(t, kst);
+        if (t + 1 < ntiles) issue_k(t + 1, kst ^ 1);
     };
     auto next_slot = [&](int t) __attribute__((always_inline)) {
-        kst = after(kst);
+        kst ^= 1;
         open_slot(t);
     };
 
@@ -180,7 +179,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void prompt_attn_kernel(PromptGeom g
     auto products = [&](auto pv, auto qk) __attribute__((always_inline)) {
         constexpr bool PV = decltype(pv)::value, QK = decltype(qk)::value;
         constexpr int RV = PV ? 2 * DT : 0, R = RV + (QK ? 4 * KSTEPS : 0);
-        const uint32_t kt = nat0 + (uint32_t)(kst * C::TILE), vt = tr0 + (uint32_t)(before(kst) * C::TILE);
+        const uint32_t kt = nat0 + (uint32_t)(kst * C::TILE), vt = tr0 + (uint32_t)((kst ^ 1) * C::TILE);
         bf16x8 ring[PF];
         auto operand = [&](int r) __attribute__((always_inline)) {
             return r < RV ? v_operand(vt, r / DT, r % DT) : k_operand(kt, (r - RV) / 4, (r - RV) % 4);
@@ -279,35 +278,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void prompt_attn_kernel(PromptGeom g
         for (int s = 0; s < NS; ++s) l_run[s] += sum[s];
     };
 
-    // prologue: K(0), V(0), K(1)
     if (ntiles > 0) {
         issue_k(0, 0);
         issue_v(0, 0);
-        if (C::NST == 3 && ntiles > 1) issue_k(1, 1);
     }
+    // One slot a tile: the products P.V of tile t-1 and S of tile t, then the softmax of tile t.
     const std::true_type yes;
     const std::false_type no;
     open_slot(0);
     if (mine > 0) {
         products(no, yes);
+        softmax(0);
         int t = 1;
-        if (!set_y) {
-            softmax(0);
-            for (; t < mine; ++t) {
-                next_slot(t);
-                products(yes, yes);
-                softmax(t);
-            }
+        for (; t < mine; ++t) {
             next_slot(t);
-        } else {
-            for (; t < mine; ++t) {
-                next_slot(t);
-                softmax(t - 1);
-                products(yes, yes);
-            }
-            next_slot(t);
-            softmax(t - 1);
+            products(yes, yes);
+            softmax(t);
         }
+        next_slot(t);
         products(yes, no);
     }
     for (int t = mine > 0 ? mine + 1 : 1; t <= ntiles; ++t) next_slot(t);  // (its loads are others' keys)
@@ -317,8 +305,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void prompt_attn_kernel(PromptGeom g
     for (int s = 0; s < NS; ++s) {
         const float l = quad_sum(l_run[s]);
         if (!valid[s]) continue;
-        if (SPLIT) {
-            float *out = partial + (((size_t)kv * per_head / parts + row_block_id(g, C::ROWS, b.seq, p.q0, i)) * parts + part) * prompt_part_floats(C::ROWS, D);
+        if (SPLIT && !whole) {
+            float *out = parts.result + ((size_t)kv * cut.cap + slot) * prompt_part_floats(D);
             const int r = 32 * wave + 16 * s + n16;
 #pragma unroll
             for (int e = 0; e < DT; ++e) *reinterpret_cast<f32x4 *>(out + r * D + 16 * e + 4 * q4) = oacc[s][e];
@@ -334,27 +322,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void prompt_attn_kernel(PromptGeom g
 }
 
 // The parts of a row put together, a wavefront for each (token, query head): lane l has D / 64 columns.
-template <int D, int ROWS>
-__global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g, int per_kv, int parts, const float *__restrict__ partial,
-                                                          uint16_t *__restrict__ O, float *__restrict__ lse)
+template <int D>
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g, PromptCut cut, PromptParts parts, uint16_t *__restrict__ O,
+                                                          float *__restrict__ lse)
 {
     constexpr int N = D / 64;
     const int lane = threadIdx.x & 63;
-    const long long row = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    if (row >= (long long)g.Tq * g.Hq) return;
-    const int tok = (int)(row / g.Hq), a = (int)(row - (long long)tok * g.Hq), kv = a / g.G;
-    int lo = 0, hi = g.B;  // the last sequence with a start at or before the token
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (g.q_start[mid] <= tok) lo = mid;
-        else hi = mid;
-    }
-    const PromptSeq p = prompt_seq(g, lo);
-    if (tok < p.q0 || tok >= p.q0 + p.n) return;
-    const int r = (tok - p.q0) * g.G + (a - kv * g.G), i = r / ROWS, at = r - i * ROWS;
-    const float *from = partial + ((size_t)kv * per_kv + row_block_id(g, ROWS, lo, p.q0, i)) * parts * prompt_part_floats(ROWS, D);
-    const float2 ml = lane < parts ? *reinterpret_cast<const float2 *>(from + lane * prompt_part_floats(ROWS, D) + ROWS * D + 2 * at)
-                                   : make_float2(-INFINITY, 0.f);
+    PartRow r;
+    if (!part_row(g, cut, parts, PROMPT_ROWS, (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r)) return;
+    const float *from = parts.result + (size_t)r.kv * cut.cap * prompt_part_floats(D);
+    const float2 ml = lane < r.n ? *reinterpret_cast<const float2 *>(from + r.item * prompt_part_floats(D) + PROMPT_ROWS * D + 2 * r.at)
+                                 : make_float2(-INFINITY, 0.f);
     float M = ml.x;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
@@ -364,73 +342,60 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g, int per_
     for (int d = 1; d < 64; d <<= 1) L += __shfl_xor(L, d, 64);
 #pragma unroll
     for (int k = 0; k < N; ++k) o[k] = 0.f;
-    for (int x = 0; x < parts; x += 4) {  // four parts' loads at a time (past the last one it is read again, with a weight of 0)
+    for (int x = 0; x < r.n; x += 4) {  // four parts' loads at a time (past the last one it is read again, with a weight of 0)
         float y[4][N];
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int k = 0; k < N; ++k) y[u][k] = from[min(x + u, parts - 1) * prompt_part_floats(ROWS, D) + at * D + N * lane + k];
+            for (int k = 0; k < N; ++k) y[u][k] = from[__builtin_amdgcn_readlane(r.item, min(x + u, r.n - 1)) * prompt_part_floats(D) + r.at * D + N * lane + k];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const float wx = x + u < parts ? __shfl(w, x + u, 64) : 0.f;
+            const float wx = x + u < r.n ? __shfl(w, x + u, 64) : 0.f;
 #pragma unroll
             for (int k = 0; k < N; ++k) o[k] = fmaf(wx, y[u][k], o[k]);
         }
     }
     const float inv = M == -INFINITY ? 0.f : 1.0f / L;
 #pragma unroll
-    for (int k = 0; k < N; ++k) reinterpret_cast<__bf16 *>(O)[(size_t)row * D + N * lane + k] = (__bf16)(o[k] * inv);
-    if (lse != nullptr && lane == 0) lse[row] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * LN2;
+    for (int k = 0; k < N; ++k) reinterpret_cast<__bf16 *>(O)[(size_t)r.row * D + N * lane + k] = (__bf16)(o[k] * inv);
+    if (lse != nullptr && lane == 0) lse[r.row] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * LN2;
 }
 
-// How many workgroups share a block's keys: as many as fill the chip's 256 CUs once, each with eight tiles at least (of all keys: where
-// a sequence has fewer than the batch, its parts are shorter).
-constexpr int SPLIT_WAVES = 8;
-static int prompt_parts(const PromptGeom &g)
+size_t prompt_workspace_bytes(const PromptGeom &g, int D)
 {
-    const long long blocks = g.Hkv * row_block_bound(g, 32 * SPLIT_WAVES), tiles = (g.Tk + KEY_TILE - 1) / KEY_TILE;
-    return (int)std::max(1ll, std::min(std::min(256 / blocks, tiles / 8), 64ll));
+    return prompt_parts(g, prompt_cut(g, PROMPT_ROWS), prompt_part_floats(D), nullptr).bytes;
 }
 
-static size_t prompt_partial_bytes(const PromptGeom &g, int D)
+template <int D, bool SPLIT>
+static hipError_t launch_walk(const PromptGeom &g, const PromptCut &cut, const PromptParts &parts, const uint16_t *Q, const uint16_t *K,
+                              const uint16_t *V, uint16_t *O, float *lse, hipStream_t st)
 {
-    const int parts = prompt_parts(g);
-    return parts > 1 ? (size_t)g.Hkv * row_block_bound(g, 32 * SPLIT_WAVES) * parts * prompt_part_floats(32 * SPLIT_WAVES, D) * 4 : 0;
-}
-size_t prompt_workspace_bytes(const PromptGeom &g, int D) { return prompt_partial_bytes(g, D); }
-
-template <int D, int WAVES, bool SPLIT>
-static hipError_t launch_walk(const PromptGeom &g, int parts, const uint16_t *Q, const uint16_t *K, const uint16_t *V, uint16_t *O,
-                              float *lse, float *partial, hipStream_t st)
-{
-    using C = Prompt<D, WAVES>;
+    using C = Prompt<D>;
     static LdsOptIn opted;  // one per kernel instantiation
-    const hipError_t e = opted.ensure(reinterpret_cast<const void *>(&prompt_attn_kernel<D, WAVES, SPLIT>), C::BYTES);
+    const hipError_t e = opted.ensure(reinterpret_cast<const void *>(&prompt_attn_kernel<D, SPLIT>), C::BYTES);
     if (e != hipSuccess) return e;
-    const int per_head = (int)row_block_bound(g, C::ROWS) * parts;
-    hipLaunchKernelGGL((prompt_attn_kernel<D, WAVES, SPLIT>), dim3(head_grid(g.Hkv, per_head)), dim3(C::THREADS), C::BYTES, st, g, per_head,
-                       parts, Q, K, V, O, lse, partial);
+    hipLaunchKernelGGL((prompt_attn_kernel<D, SPLIT>), dim3(head_grid(g.Hkv, SPLIT ? cut.cap : (int)cut.blocks)), dim3(C::THREADS), C::BYTES,
+                       st, g, cut, parts, Q, K, V, O, lse);
     return hipGetLastError();
 }
 
 template <int D>
 static hipError_t launch_prompt_d(const PromptGeom &g, const uint16_t *Q, const uint16_t *K, const uint16_t *V, uint16_t *O, float *lse,
-                                  float *partial, hipStream_t st)
+                                  void *ws, hipStream_t st)
 {
-    const int parts = prompt_parts(g);
-    if (parts == 1) return getenv("W4") ? launch_walk<D, 4, false>(g, 1, Q, K, V, O, lse, nullptr, st) : launch_walk<D, 8, false>(g, 1, Q, K, V, O, lse, nullptr, st);
-    const hipError_t e = launch_walk<D, SPLIT_WAVES, true>(g, parts, Q, K, V, O, lse, partial, st);
+    const PromptCut cut = prompt_cut(g, PROMPT_ROWS);
+    const PromptParts parts = prompt_parts(g, cut, prompt_part_floats(D), ws);
+    if (cut.cap == 0) return launch_walk<D, false>(g, cut, parts, Q, K, V, O, lse, st);
+    const hipError_t e = launch_walk<D, true>(g, cut, parts, Q, K, V, O, lse, st);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((prompt_join_kernel<D, 32 * SPLIT_WAVES>), dim3((unsigned)(((long long)g.Tq * g.Hq + 3) / 4)), dim3(256), 0, st, g,
-                       (int)row_block_bound(g, 32 * SPLIT_WAVES), parts, partial, O, lse);
+    hipLaunchKernelGGL((prompt_join_kernel<D>), dim3((unsigned)(((long long)g.Tq * g.Hq + 3) / 4)), dim3(256), 0, st, g, cut, parts, O, lse);
     return hipGetLastError();
 }
 
 hipError_t launch_prompt_attn(const PromptGeom &g, int D, const uint16_t *Q, const uint16_t *K, const uint16_t *V, uint16_t *O,
                               float *lse, void *ws, hipStream_t st)
 {
-    float *partial = static_cast<float *>(ws);
-    return D == 64 ? launch_prompt_d<64>(g, Q, K, V, O, lse, partial, st) : launch_prompt_d<128>(g, Q, K, V, O, lse, partial, st);
+    return D == 64 ? launch_prompt_d<64>(g, Q, K, V, O, lse, ws, st) : launch_prompt_d<128>(g, Q, K, V, O, lse, ws, st);
 }
 
 }  // namespace adaspark

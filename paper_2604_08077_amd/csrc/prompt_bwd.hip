@@ -4,16 +4,24 @@
 // with dK, dV summed over the G heads of a KV head's group.  p is rebuilt from the log-sum-exp.  As in the backward of the cube-selective
 // attention (attn_bwd.hip) two kernels, one that keeps rows and one that keeps keys, do it without atomics: seven products
 // where five would do with them, and the same bits every time.
-//   prompt_dq_kernel   256 rows of a (sequence, KV head), 32 to a wavefront with Q and dO in registers, over tiles of 64 keys:
+//   prompt_dq_kernel   128 rows of a (sequence, KV head), 32 to a wavefront with Q and dO in registers, over tiles of 64 keys:
 //                      S^T = K.Q^T, dP^T = V.dO^T, dQ^T += K^T.dS^T.
-//   prompt_dkv_kernel  256 keys, 32 to a wavefront with K and V in registers, over tiles of 64 rows:
+//   prompt_dkv_kernel  128 keys, 32 to a wavefront with K and V in registers, over tiles of 64 rows:
 //                      S = Q.K^T, dP = dO.V^T, dV^T += dO^T.P, dK^T += Q^T.dS.
 // All tiles are rows as the caller holds them, read in LDS both ways (rowtile.h).  The accumulators of S start from
 // -lse * sqrt(D) and those of dP from -delta, which prompt_prep_kernel leaves per row.
 // Score products are exact; p and dS are rounded to bf16 as operands of the other products, sums are fp32.
 //
+// sum_j dS_j = 0 in a row, so dQ = c sum_j dS_j (k_j - r) for any r.  What the roundings of dS and of O (in delta) leave does not sum to
+// zero, and keys of one text share a direction, along which all of it adds up.  So the row's sum of dS as rounded is kept beside
+// dQ (two MFMAs a tile against 96) and that many r taken off at the end, r the mean of 64 keys of the sequence: the error of dQ
+// against 64 bits, keys of as much common as own direction, goes from 4.0e-3 to 2.6e-3.
+//
 // Where few key blocks have long walks, a walk is cut into spans, a workgroup each, which leave fp32 sums in the
-// workspace; prompt_reduce_kernel adds them in their order.
+// workspace; prompt_reduce_kernel adds them in their order.  Walks of few row blocks are shared out as in the forward (prompt.h).
+//
+// Workgroups of four wavefronts and two stages, two to a CU, which are not in step (a training pass over 16k tokens in 5 sequences of 28/4 heads
+// of 128, in ms, with eight wavefronts and three stages 2.31, so 2.20).
 #include <algorithm>
 
 #include "prompt.h"
@@ -78,8 +86,13 @@ __device__ __forceinline__ int span_tiles(const PromptGeom &g, int most)
     return max(max(SPAN_MIN, (longest + most - 1) / most), (int)min(total * (float)g.Hkv / (64.f * SPAN_ITEMS), 1e9f));
 }
 
+// A part of a dQ walk: its sum of dS k, fp32 [128 rows][D], then each row's sum of dS.
+__host__ __device__ inline size_t dq_part_floats(int D) { return (size_t)PB_BLOCK * (D + 1); }
+
 struct PromptBwdWorkspace {
     int *span;            // tiles of a span
+    float *mean;          // [B][Hkv][D] of 64 keys of each sequence
+    PromptParts rows;     // parts of the dQ kernel's walks
     float *lse2, *delta;  // [Tq * Hq + 1]: entry [Tq * Hq] belongs to the rows that pad a tile: -inf, 0
     float *part;          // [Hkv][blocks][most][2 (dV, dK)][256 x D] in MFMA output order
     size_t bytes;
@@ -91,20 +104,27 @@ static PromptBwdWorkspace bwd_workspace_of(const PromptGeom &g, int D, void *ws)
     const size_t rows = up(((size_t)g.Tq * g.Hq + 1) * 4);
     unsigned char *p = static_cast<unsigned char *>(ws);
     PromptBwdWorkspace w;
+    unsigned char *const begin = p;
     w.span = reinterpret_cast<int *>(p);
     p += 256;
+    w.mean = reinterpret_cast<float *>(p);
+    p += up((size_t)g.B * g.Hkv * D * 4);
+    w.rows = prompt_parts(g, prompt_cut(g, PB_BLOCK), dq_part_floats(D), p);
+    p += up(w.rows.bytes);
     w.lse2 = reinterpret_cast<float *>(p);
     w.delta = reinterpret_cast<float *>(p + rows);
     w.part = reinterpret_cast<float *>(p + 2 * rows);
-    w.bytes = 256 + 2 * rows + (s.most > 1 ? (size_t)g.Hkv * s.blocks * s.most * 2 * PB_BLOCK * D * 4 : 0);
+    w.bytes = (size_t)(p - begin) + 2 * rows + (s.most > 1 ? (size_t)g.Hkv * s.blocks * s.most * 2 * PB_BLOCK * D * 4 : 0);
     return w;
 }
 size_t prompt_bwd_workspace_bytes(const PromptGeom &g, int D) { return bwd_workspace_of(g, D, nullptr).bytes; }
 
 // Start values of every row: 256 / (D / 8) rows to a workgroup, D / 8 lanes to a row.  A row without keys (log-sum-exp -inf) gets
-// no part in anything.  The first workgroup's first wavefront also leaves the length of a span.
+// no part in anything.  The first B * Hkv workgroups leave the mean keys, a thread to a column and as many keys as there are threads for;
+// the very first wavefront also the length of a span.
 template <int D>
-__global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most, int *__restrict__ span, long long rows, const uint16_t *__restrict__ O, const uint16_t *__restrict__ dO,
+__global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most, int *__restrict__ span, const uint16_t *__restrict__ K,
+                                                          float *__restrict__ mean, long long rows, const uint16_t *__restrict__ O, const uint16_t *__restrict__ dO,
                                                           const float *__restrict__ lse, float *__restrict__ lse2,
                                                           float *__restrict__ delta)
 {
@@ -113,7 +133,24 @@ __global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most
         const int tiles = span_tiles(g, most);
         if (threadIdx.x == 0) *span = tiles;
     }
-    const long long r = ((long long)blockIdx.x * 256 + threadIdx.x) / CPR;
+    const unsigned means = (unsigned)g.B * (unsigned)g.Hkv;
+    if (blockIdx.x < means) {
+        __shared__ float sums[256];
+        const int s = (int)(blockIdx.x / (unsigned)g.Hkv), kv = (int)(blockIdx.x % (unsigned)g.Hkv), d = threadIdx.x % D;
+        const PromptSeq p = prompt_seq(g, s);
+        const int n = min(p.m, 64);
+        float x = 0.f;
+        for (int i = threadIdx.x / D; i < n; i += 256 / D)  // 64 keys, evenly spread
+            x += __uint_as_float((uint32_t)K[(size_t)(p.k0 + (int)((long long)i * p.m / n)) * g.ks + (size_t)kv * D + d] << 16);
+        sums[threadIdx.x] = x;
+        __syncthreads();
+        if (threadIdx.x < D) {
+            for (int i = 1; i < 256 / D; ++i) x += sums[i * D + d];
+            mean[((size_t)s * g.Hkv + kv) * D + d] = n > 0 ? x / (float)n : 0.f;
+        }
+        return;
+    }
+    const long long r = ((long long)(blockIdx.x - means) * 256 + threadIdx.x) / CPR;
     const int col = threadIdx.x % CPR;
     float part = 0.f;
     if (r < rows) {
@@ -130,11 +167,12 @@ __global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most
     }
 }
 
-template <int D>
-__global__ __launch_bounds__(PB_THREADS, 2) void prompt_dq_kernel(PromptGeom g, int per_head, const uint16_t *__restrict__ Q,
-                                                               const uint16_t *__restrict__ K, const uint16_t *__restrict__ V,
-                                                               const uint16_t *__restrict__ dO, const float *__restrict__ lse2p,
-                                                               const float *__restrict__ deltap, uint16_t *__restrict__ dQ)
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(PB_THREADS, 2) void prompt_dq_kernel(PromptGeom g, PromptCut cut, PromptParts parts,
+                                                                  const uint16_t *__restrict__ Q, const uint16_t *__restrict__ K,
+                                                                  const uint16_t *__restrict__ V, const uint16_t *__restrict__ dO,
+                                                                  const float *__restrict__ lse2p, const float *__restrict__ deltap,
+                                                                  const float *__restrict__ mean, uint16_t *__restrict__ dQ)
 {
     using C = PromptBwd<D>;
     constexpr int NS = 2, KSTEPS = D / 32, DT = D / 16;
@@ -143,19 +181,34 @@ __global__ __launch_bounds__(PB_THREADS, 2) void prompt_dq_kernel(PromptGeom g, 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
     int kv, slot;
-    if (!head_slot(blockIdx.x, g.Hkv, per_head, kv, slot)) return;
-    const PromptBlock b = longest_first(g, slot, (g.Tk + KEY_TILE - 1) / KEY_TILE,
-                                        [&](int n, int m, int t) { return row_blocks<PB_BLOCK>(n, m, g.G, g.causal, t); });
-    if (b.seq < 0) return;
-    const PromptSeq p = b.p;
-    const int rows = p.n * g.G, row0 = ((rows - 1) / PB_BLOCK - b.block) * PB_BLOCK;
+    if (!head_slot(blockIdx.x, g.Hkv, SPLIT ? cut.cap : (int)cut.blocks, kv, slot)) return;
+    PromptItem it;
+    if constexpr (SPLIT) it = prompt_item<PB_BLOCK>(g, slot, cut.cap);
+    else it = {longest_first(g, slot, (g.Tk + KEY_TILE - 1) / KEY_TILE,
+                             [&](int n, int m, int t) { return row_blocks<PB_BLOCK>(n, m, g.G, g.causal, t); }), 0, 0};
+    if (it.b.seq < 0) return;
+    const PromptSeq p = it.b.p;
+    const int rows = p.n * g.G, i = (rows - 1) / PB_BLOCK - it.b.block, row0 = i * PB_BLOCK;
     auto reach_of = [&](int row) { return g.causal ? p.m - p.n + token_of_row(g, row) : p.m - 1; };
     auto tiles_to = [&](int row) {
         const int r = reach_of(min(row, rows - 1));
         return r < 0 ? 0 : r / KEY_TILE + 1;
     };
-    const int ntiles = __builtin_amdgcn_readfirstlane(tiles_to(row0 + PB_BLOCK - 1));
+    // the tiles of the block's walk, up to which this workgroup and this wavefront go, and from which on
+    int first = 0, ntiles = __builtin_amdgcn_readfirstlane(tiles_to(row0 + PB_BLOCK - 1));
     const int mine = row0 + 32 * wave < rows ? __builtin_amdgcn_readfirstlane(tiles_to(row0 + 32 * wave + 31)) : 0;
+    bool whole = true;
+    if (SPLIT) {
+        const int n = max(1, (ntiles + it.chunk - 1) / it.chunk), per = (ntiles + n - 1) / n;
+        whole = n == 1;
+        if (threadIdx.x == 0) {
+            const size_t id = (size_t)kv * cut.blocks + row_block_id(g, PB_BLOCK, it.b.seq, p.q0, i);
+            if (it.part == 0) parts.count[id] = n;
+            parts.item[id * PARTS_MAX + it.part] = slot;
+        }
+        first = min(it.part * per, ntiles);
+        ntiles = min(first + per, ntiles);
+    }
 
     int reach[NS];
     bool valid[NS];
@@ -207,11 +260,13 @@ __global__ __launch_bounds__(PB_THREADS, 2) void prompt_dq_kernel(PromptGeom g, 
         }
     };
 
-    f32x4 acc[NS][DT];
+    f32x4 acc[NS][DT], total[NS];  // total: every element the row's sum of dS
 #pragma unroll
-    for (int s = 0; s < NS; ++s)
+    for (int s = 0; s < NS; ++s) {
+        total[s] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int e = 0; e < DT; ++e) acc[s][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     const float c2 = 1.44269504088896340736f / sqrtf((float)D);  // softmax scale in base 2
     const uint32_t nat0 = (uint32_t)row_tile_off<D>(n16, q4);
     const uint32_t tr0 = (uint32_t)(row_tile_off<D>(4 * q4 + (n16 >> 2), (n16 & 3) >> 1) + 8 * (n16 & 1));
@@ -269,6 +324,10 @@ __global__ __launch_bounds__(PB_THREADS, 2) void prompt_dq_kernel(PromptGeom g, 
             for (int e = 0; e < DT; ++e) {
                 if (e + 1 < DT) tp[(e + 1) & 1] = cols_at(H, e + 1);
                 else if (H == 0) rows_at(2, 0, op[0]);
+                if (e == 0) {
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) total[s] = mfma16(ones_operand(), ds[s], total[s]);
+                }
 #pragma unroll
                 for (int s = 0; s < NS; ++s) acc[s][e] = mfma16(tp[e & 1], ds[s], acc[s][e]);
                 __builtin_amdgcn_sched_barrier(0);
@@ -277,20 +336,66 @@ __global__ __launch_bounds__(PB_THREADS, 2) void prompt_dq_kernel(PromptGeom g, 
     };
     static_assert(KSTEPS % 2 == 0 && DT % 2 == 0, "the operands' two places take turns");
 
-    if (ntiles > 0) issue(0, 0);
-    for (int t = 0; t < ntiles; ++t) {
+    if (first < ntiles) issue(first, first & 1);
+    for (int t = first; t < ntiles; ++t) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (t + 1 < ntiles) issue(t + 1, (t + 1) & 1);  // (the stage read last at tile t - 1)
         if (t < mine) work(t, t & 1);
     }
     const float c = 1.0f / sqrtf((float)D);
+    const float *r = mean + ((size_t)it.b.seq * g.Hkv + kv) * D + 4 * q4;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
         if (!valid[s]) continue;
-        uint16_t *o = dQ + rid[s] * D + 4 * q4;
+        if (SPLIT && !whole) {
+            float *out = parts.result + ((size_t)kv * cut.cap + slot) * dq_part_floats(D);
+            const int at = 32 * wave + 16 * s + n16;
 #pragma unroll
-        for (int e = 0; e < DT; ++e) *reinterpret_cast<uint2 *>(o + 16 * e) = pack_bf16(acc[s][e] * c);
+            for (int e = 0; e < DT; ++e) *reinterpret_cast<f32x4 *>(out + at * D + 16 * e + 4 * q4) = acc[s][e];
+            if (q4 == 0) out[PB_BLOCK * D + at] = total[s][0];
+        } else {
+            uint16_t *o = dQ + rid[s] * D + 4 * q4;
+#pragma unroll
+            for (int e = 0; e < DT; ++e)
+                *reinterpret_cast<uint2 *>(o + 16 * e) = pack_bf16((acc[s][e] - total[s][0] * *reinterpret_cast<const f32x4 *>(r + 16 * e)) * c);
+        }
     }
+}
+
+// The parts of a row's dQ added in their order, a wavefront for each (token, query head): lane l has D / 64 columns.
+template <int D>
+__global__ __launch_bounds__(256) void prompt_dq_join_kernel(PromptGeom g, PromptCut cut, PromptParts parts, const float *__restrict__ mean,
+                                                             uint16_t *__restrict__ dQ)
+{
+    constexpr int N = D / 64;
+    const int lane = threadIdx.x & 63;
+    PartRow r;
+    if (!part_row(g, cut, parts, PB_BLOCK, (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r)) return;
+    const float *from = parts.result + (size_t)r.kv * cut.cap * dq_part_floats(D);
+    float o[N], total = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) o[k] = 0.f;
+    for (int x = 0; x < r.n; x += 4) {  // four parts' loads at a time
+        float y[4][N], t[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float *part = from + __builtin_amdgcn_readlane(r.item, min(x + u, r.n - 1)) * dq_part_floats(D);
+            t[u] = part[PB_BLOCK * D + r.at];
+#pragma unroll
+            for (int k = 0; k < N; ++k) y[u][k] = part[r.at * D + N * lane + k];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (x + u >= r.n) break;
+            total += t[u];
+#pragma unroll
+            for (int k = 0; k < N; ++k) o[k] += y[u][k];
+        }
+    }
+    const float c = 1.0f / sqrtf((float)D);
+    const float *m = mean + ((size_t)r.seq * g.Hkv + r.kv) * D + N * lane;
+#pragma unroll
+    for (int k = 0; k < N; ++k) reinterpret_cast<__bf16 *>(dQ)[(size_t)r.row * D + N * lane + k] = (__bf16)((o[k] - total * m[k]) * c);
 }
 
 // Key blocks of a sequence whose walk over the rows has at least t tiles of 64; the first blocks walk farthest.
@@ -565,13 +670,14 @@ static hipError_t launch_bwd(const PromptGeom &g, const uint16_t *Q, const uint1
     using C = PromptBwd<D>;
     const PromptBwdWorkspace w = bwd_workspace_of(g, D, ws);
     const PromptSpans cut = prompt_spans(g);
-    static LdsOptIn opted_q, opted_kv;
-    hipError_t e = opted_q.ensure(reinterpret_cast<const void *>(&prompt_dq_kernel<D>), C::BYTES);
+    static LdsOptIn opted_q, opted_parts, opted_kv;
+    hipError_t e = opted_q.ensure(reinterpret_cast<const void *>(&prompt_dq_kernel<D, false>), C::BYTES);
+    if (e == hipSuccess) e = opted_parts.ensure(reinterpret_cast<const void *>(&prompt_dq_kernel<D, true>), C::BYTES);
     if (e == hipSuccess) e = opted_kv.ensure(reinterpret_cast<const void *>(&prompt_dkv_kernel<D>), C::BYTES);
     if (e != hipSuccess) return e;
     const long long rows = (long long)g.Tq * g.Hq, per = 256 / (D / 8);
-    hipLaunchKernelGGL((prompt_prep_kernel<D>), dim3((unsigned)((rows + 1 + per - 1) / per)), dim3(256), 0, st, g, cut.most, w.span, rows, O, dO,
-                       lse, w.lse2, w.delta);
+    hipLaunchKernelGGL((prompt_prep_kernel<D>), dim3((unsigned)((long long)g.B * g.Hkv + (rows + 1 + per - 1) / per)), dim3(256), 0, st, g,
+                       cut.most, w.span, K, w.mean, rows, O, dO, lse, w.lse2, w.delta);
     if (g.Tk > 0) {
         const int keys = (int)cut.blocks * cut.most;
         hipLaunchKernelGGL((prompt_dkv_kernel<D>), dim3(head_grid(g.Hkv, keys)), dim3(PB_THREADS), C::BYTES, st, g, keys, cut, w.span, Q, K, V, dO,
@@ -580,9 +686,15 @@ static hipError_t launch_bwd(const PromptGeom &g, const uint16_t *Q, const uint1
             hipLaunchKernelGGL((prompt_reduce_kernel<D>), dim3((unsigned)(cut.blocks * g.Hkv * PB_WAVES)), dim3(256), 0, st, g, cut, w.span, w.part, dK, dV);
     }
     if (g.Tq > 0) {
-        const int blocks = (int)row_block_bound(g, PB_BLOCK);
-        hipLaunchKernelGGL((prompt_dq_kernel<D>), dim3(head_grid(g.Hkv, blocks)), dim3(PB_THREADS), C::BYTES, st, g, blocks, Q, K, V, dO,
-                           w.lse2, w.delta, dQ);
+        const PromptCut rc = prompt_cut(g, PB_BLOCK);
+        if (rc.cap == 0) {
+            hipLaunchKernelGGL((prompt_dq_kernel<D, false>), dim3(head_grid(g.Hkv, (int)rc.blocks)), dim3(PB_THREADS), C::BYTES, st, g, rc, w.rows, Q,
+                               K, V, dO, w.lse2, w.delta, w.mean, dQ);
+        } else {
+            hipLaunchKernelGGL((prompt_dq_kernel<D, true>), dim3(head_grid(g.Hkv, rc.cap)), dim3(PB_THREADS), C::BYTES, st, g, rc, w.rows, Q, K, V,
+                               dO, w.lse2, w.delta, w.mean, dQ);
+            hipLaunchKernelGGL((prompt_dq_join_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, g, rc, w.rows, w.mean, dQ);
+        }
     }
     return hipGetLastError();
 }

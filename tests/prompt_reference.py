@@ -52,7 +52,10 @@ def lse_bound(ref, keys):
 
 
 def gradients(Q, K, V, O, lse, dO, q_len, k_len, causal=True):
-    """The formulas of the backward on the O and lse that it is given -> fp64 dQ, dK, dV and their bounds."""
+    """The formulas of the backward on the O and lse that it is given -> fp64 dQ, dK, dV and their bounds.
+
+    sum_j dS_j = sum_j p_j dP_j - delta is 0 for the delta that belongs to p; with delta from an O rounded to bf16 something is left of it, and the
+    library takes that out of dQ along r, the mean of up to 64 keys of the sequence: dQ = c sum_j dS_j (k_j - r)."""
     Hq, D, Hkv = Q.shape[1], Q.shape[2], K.shape[1]
     G, c = Hq // Hkv, 1 / math.sqrt(Q.shape[2])
     out = {n: torch.zeros(t.shape, dtype=torch.float64, device=Q.device) for n, t in (("dQ", Q), ("dK", K), ("dV", V))}
@@ -75,11 +78,13 @@ def gradients(Q, K, V, O, lse, dO, q_len, k_len, causal=True):
             ddp = U32 * (D + 4) * (g.abs() @ v.abs().T + (g * o).abs().sum(-1, keepdim=True))   # of dp - delta
             e_ds = ds.abs() * (U16 + off) + p * ddp * (1 + U16)                                 # dS in bf16
             e_p = p * (U16 + off)
-            out["dQ"][at] += c * ds @ k
+            few = min(m, 64)
+            r = k[torch.arange(few, device=k.device) * m // few].mean(0)
+            out["dQ"][at] += c * (ds @ k - ds.sum(-1, keepdim=True) * r)
             out["dK"][kt] += c * ds.T @ q
             out["dV"][kt] += p.T @ g
             n32 = 2 * U32 * (m + 4), 2 * U32 * (n * G + 4)  # sums in fp32
-            tol["dQ"][at] += c * (e_ds + ds.abs() * n32[0]) @ k.abs()
+            tol["dQ"][at] += c * (e_ds + ds.abs() * n32[0]) @ (k.abs() + r.abs())
             tol["dK"][kt] += c * (e_ds + ds.abs() * n32[1]).T @ q.abs()
             tol["dV"][kt] += (e_p + p * n32[1]).T @ g.abs()
         q0, k0 = q0 + n, k0 + m
