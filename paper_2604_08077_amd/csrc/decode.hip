@@ -4,9 +4,10 @@
 // Every key and value is read once and meets the query heads of its KV head only, so the time is that of reading them from
 // HBM: 4 * G FLOP per byte of bf16, which leaves the matrix pipes nearly idle, and the wavefronts' one task is to keep
 // enough bytes in flight.  A workgroup takes a part of one sequence's keys for one KV head (decode_plan: parts of one
-// length over the whole batch, as many as fill the chip), its four wavefronts every fourth tile of 8 KB of keys and 8 KB of values.
+// length over the whole batch, as many as fill the chip), its two wavefronts every second tile of 8 KB of keys and 8 KB of values.
 // A wavefront is by itself: two stages of LDS that only it fills and reads, direct-to-LDS loads of the next tile in flight
-// while it works this one, no barrier before the end, when the four partial results are put together.
+// while it works this one, no barrier before the end, when the partial results are put together.  Two workgroups on a CU: one's plan, first loads
+// and end run while the other reads.
 // Sequences of several parts leave them (fp32) in the workspace, and decode_join_kernel puts these together.
 //
 // The products are the attention kernels': S^T = K.Q^T and O^T += V^T.P^T with 16x16x32 MFMAs, a lane's column is one query
@@ -19,12 +20,13 @@ namespace adaspark {
 
 typedef int s32x2 __attribute__((ext_vector_type(2)));
 
+constexpr int DECODE_WAVES = 2;
 constexpr int DECODE_PLAN_SEQS = 512;  // sequences that a wavefront's lanes hold the lengths of, eight each
-constexpr int DECODE_CUS = 256;
+constexpr int DECODE_PLACES = 512;    // workgroups that the chip holds at once, two to a CU
 
 template <int D, bool E4M3>
 struct Decode {
-    static constexpr int WAVES = 4;
+    static constexpr int WAVES = DECODE_WAVES;
     static constexpr int THREADS = 64 * WAVES;
     static constexpr int ROW = D * (E4M3 ? 1 : 2);  // bytes of a key
     static constexpr int KEYS = 8192 / ROW;         // of a tile: 32, 64 or 128
@@ -37,7 +39,7 @@ struct Decode {
     static constexpr int PAGES = (KEYS < 64 ? 64 : KEYS) * 4;  // the page of each key of a tile
     static constexpr int WAVE_BYTES = 2 * STAGE + 2 * PAGES;
     static constexpr int BYTES = WAVES * WAVE_BYTES;
-    static_assert(BYTES <= 160 * 1024, "LDS of one CU");
+    static_assert(BYTES <= 80 * 1024, "half the LDS of a CU");
     static_assert(16 * D * 4 + 256 <= WAVE_BYTES, "a wavefront's result takes the place of its stages");
 };
 
@@ -48,15 +50,15 @@ struct DecodePart {
     int item0;           // number of the sequence's first part
     int key0, key1;
 };
-__host__ __device__ inline int decode_unit(const CacheGeom &g) { return 4 * 8192 / (g.D * (g.e4m3 ? 1 : 2)); }
+__host__ __device__ inline int decode_unit(const CacheGeom &g) { return 2 * DECODE_WAVES * 8192 / (g.D * (g.e4m3 ? 1 : 2)); }  // keys
 
-// Parts that a KV head and 16 query heads of its group get: a workgroup each, whole rounds of the chip's CUs, at least two for
+// Parts that a KV head and 16 query heads of its group get: a workgroup each, whole rounds of the chip, at least two for
 // a sequence on average -- the parts have one length, and lengths differ.
 __host__ __device__ inline int decode_parts(const CacheGeom &g)
 {
     const long long rows = (long long)g.Hkv * ((g.G + 15) / 16);
     if (g.B > DECODE_PLAN_SEQS) return g.B;
-    const long long slots = (2 * g.B * rows + DECODE_CUS - 1) / DECODE_CUS * DECODE_CUS;
+    const long long slots = (2 * g.B * rows + DECODE_PLACES - 1) / DECODE_PLACES * DECODE_PLACES;
     return (int)(slots / rows > g.B ? slots / rows : g.B);
 }
 
@@ -64,13 +66,6 @@ __device__ __forceinline__ int cache_length(const CacheGeom &g, int len)
 {
     const long long most = (long long)g.table_pages << g.shift;
     return max(0, (int)min((long long)len, most));
-}
-
-__device__ __forceinline__ int wave_sum(int x)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
-    return x;
 }
 
 // chunk of the batch: the smallest multiple of `unit` with at most `most` parts (lengths: of sequence 64 * c + lane)
@@ -99,20 +94,19 @@ __device__ __forceinline__ int decode_chunk(const int (&len)[DECODE_PLAN_SEQS / 
 #pragma unroll
         for (int c = 0; c < DECODE_PLAN_SEQS / 64; ++c)
             if (c < chunks && 64 * c + lane < B) n += max(1, (len[c] + chunk - 1) / chunk);
-        if (wave_sum(n) <= most) hi = mid;
+        if (wave_total(n) <= most) hi = mid;
         else lo = mid + 1;
     }
     return __builtin_amdgcn_readfirstlane(lo) * unit;
 }
 
-// Part number `item` of the batch (item >= 0), or with item < 0 all parts of sequence `seq`.
-__device__ __forceinline__ DecodePart decode_plan(const CacheGeom &g, const int32_t *lengths, int item, int seq)
+// Part number `item` of the batch.
+__device__ __forceinline__ DecodePart decode_plan(const CacheGeom &g, const int32_t *lengths, int item)
 {
     DecodePart p = {-1, 0, 1, 0, 0, 0};
     const int lane = threadIdx.x & 63;
     if (g.B > DECODE_PLAN_SEQS) {  // enough sequences to fill the chip: a part for each
-        p.s = item >= 0 ? item : seq;
-        p.item0 = p.s;
+        p.s = p.item0 = item;
         p.key1 = cache_length(g, lengths[p.s]);
         return p;
     }
@@ -128,20 +122,14 @@ __device__ __forceinline__ DecodePart decode_plan(const CacheGeom &g, const int3
         for (int k = 0; k < DECODE_PLAN_SEQS / 64; ++k)
             if (k == c) mine = len[k];
         const int n = 64 * c + lane < g.B ? max(1, (mine + chunk - 1) / chunk) : 0;
-        int incl = n;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(incl, d, 64);
-            if (lane >= d) incl += up;
-        }
-        const bool here = item >= 0 ? n > 0 && item >= base + incl - n && item < base + incl : 64 * c + lane == seq;
-        const unsigned long long b = __ballot(here);
+        const int incl = wave_scan(n);
+        const unsigned long long b = __ballot(item < base + incl);
         if (b != 0ull) {
             const int src = __builtin_amdgcn_readfirstlane(__ffsll(b) - 1);
             p.s = 64 * c + src;
             p.parts = __builtin_amdgcn_readlane(n, src);
             p.item0 = base + __builtin_amdgcn_readlane(incl, src) - p.parts;
-            p.part = item >= 0 ? item - p.item0 : 0;
+            p.part = item - p.item0;
             const int m = __builtin_amdgcn_readlane(mine, src);
             p.key0 = min(p.part * chunk, m);
             p.key1 = p.key0 + min(chunk, m - p.key0);
@@ -175,17 +163,20 @@ __device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t a, uint32_t b)
     return bf16x8{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
 }
 
-// A part's result: O unnormalised, fp32 [16 heads][D], then m and l (base 2) of each head.
+// A part's result: O unnormalised, fp32 [16 heads][D], then m and l (base 2) of each head.  Before the results, in the workspace,
+// what decode_join_kernel goes by: each sequence's first part and how many there are.
 __host__ __device__ inline size_t decode_part_floats(int D) { return 16 * (size_t)D + 32; }
+__host__ __device__ inline size_t decode_plan_bytes(const CacheGeom &g) { return ((size_t)g.B * 8 + 255) & ~(size_t)255; }
 
 template <int D, bool E4M3>
-__global__ __launch_bounds__(256) void decode_attn_kernel(CacheGeom g, const uint16_t *__restrict__ Q,
+__global__ __launch_bounds__(64 * DECODE_WAVES) void decode_attn_kernel(CacheGeom g, const uint16_t *__restrict__ Q,
                                                           const int32_t *__restrict__ table,
                                                           const int32_t *__restrict__ lengths,
                                                           const unsigned char *__restrict__ Kc,
                                                           const unsigned char *__restrict__ Vc, const float *__restrict__ ks,
                                                           const float *__restrict__ vs, uint16_t *__restrict__ O,
-                                                          float *__restrict__ lse, float *__restrict__ parts)
+                                                          float *__restrict__ lse, int2 *__restrict__ plan,
+                                                          float *__restrict__ parts)
 {
     using C = Decode<D, E4M3>;
     constexpr int KEYS = C::KEYS, KG = KEYS / 16, KSTEPS = D / 32, DT = D / 16;
@@ -196,8 +187,9 @@ __global__ __launch_bounds__(256) void decode_attn_kernel(CacheGeom g, const uin
     const int groups = (g.G + 15) / 16, heads = g.Hkv * groups;
     const int item = (int)(blockIdx.x / (unsigned)heads), hh = (int)(blockIdx.x % (unsigned)heads);
     const int kv = hh / groups, head0 = kv * g.G + hh % groups * 16, nheads = min(16, (kv + 1) * g.G - head0);
-    const DecodePart p = decode_plan(g, lengths, item, 0);
+    const DecodePart p = decode_plan(g, lengths, item);
     if (p.s < 0) return;
+    if (plan != nullptr && p.part == 0 && hh == 0 && threadIdx.x == 0) plan[p.s] = make_int2(p.item0, p.parts);
 
     // Q operands: MFMA k index 8 q4 + e of step c is d = 32 c + 8 q4 + e; in 8 bits, where a lane reads 16 codes at a time for
     // two steps, step 2 c + u has d = 64 c + 16 q4 + 8 u + e.
@@ -408,7 +400,7 @@ __global__ __launch_bounds__(256) void decode_attn_kernel(CacheGeom g, const uin
 
 // The parts of a sequence put together, a wavefront for each (sequence, query head): lane l has D / 64 columns.
 template <int D>
-__global__ __launch_bounds__(256) void decode_join_kernel(CacheGeom g, const int32_t *__restrict__ lengths,
+__global__ __launch_bounds__(256) void decode_join_kernel(CacheGeom g, const int2 *__restrict__ plan,
                                                           const float *__restrict__ parts, uint16_t *__restrict__ O,
                                                           float *__restrict__ lse)
 {
@@ -417,7 +409,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(CacheGeom g, const int
     const int row = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
     if (row >= g.B * g.Hq) return;
     const int s = row / g.Hq, a = row - s * g.Hq;
-    const DecodePart p = decode_plan(g, lengths, -1, s);
+    struct { int item0, parts; } p = {plan[s].x, plan[s].y};
     if (p.parts <= 1) return;
     const int groups = (g.G + 15) / 16, heads = g.Hkv * groups;
     const int kv = a / g.G, hh = kv * groups + (a - kv * g.G) / 16, col = (a - kv * g.G) & 15;
@@ -467,34 +459,36 @@ __global__ __launch_bounds__(256) void decode_join_kernel(CacheGeom g, const int
 size_t decode_workspace_bytes(const CacheGeom &g)
 {
     const int parts = decode_parts(g);
-    return parts > g.B ? (size_t)parts * g.Hkv * ((g.G + 15) / 16) * decode_part_floats(g.D) * 4 : 0;
+    return parts > g.B ? decode_plan_bytes(g) + (size_t)parts * g.Hkv * ((g.G + 15) / 16) * decode_part_floats(g.D) * 4 : 0;
 }
 
 template <int D, bool E4M3>
 static hipError_t launch_decode(const CacheGeom &g, const uint16_t *Q, const int32_t *table, const int32_t *lengths,
-                                const CacheData &c, uint16_t *O, float *lse, float *parts, hipStream_t st)
+                                const CacheData &c, uint16_t *O, float *lse, void *ws, hipStream_t st)
 {
     using C = Decode<D, E4M3>;
     static LdsOptIn opted;  // one per kernel instantiation
     const hipError_t e = opted.ensure(reinterpret_cast<const void *>(&decode_attn_kernel<D, E4M3>), C::BYTES);
     if (e != hipSuccess) return e;
+    const bool shared = decode_parts(g) > g.B;
+    int2 *plan = shared ? static_cast<int2 *>(ws) : nullptr;
+    float *parts = shared ? reinterpret_cast<float *>(static_cast<char *>(ws) + decode_plan_bytes(g)) : nullptr;
     const unsigned heads = (unsigned)(g.Hkv * ((g.G + 15) / 16));
     hipLaunchKernelGGL((decode_attn_kernel<D, E4M3>), dim3((unsigned)decode_parts(g) * heads), dim3(C::THREADS), C::BYTES, st, g, Q,
                        table, lengths, static_cast<const unsigned char *>(c.K), static_cast<const unsigned char *>(c.V), c.ks,
-                       c.vs, O, lse, parts);
-    if (decode_parts(g) > g.B)
-        hipLaunchKernelGGL((decode_join_kernel<D>), dim3((unsigned)((g.B * g.Hq + 3) / 4)), dim3(256), 0, st, g, lengths, parts, O, lse);
+                       c.vs, O, lse, plan, parts);
+    if (shared)
+        hipLaunchKernelGGL((decode_join_kernel<D>), dim3((unsigned)((g.B * g.Hq + 3) / 4)), dim3(256), 0, st, g, plan, parts, O, lse);
     return hipGetLastError();
 }
 
 hipError_t launch_decode_attn(const CacheGeom &g, const uint16_t *Q, const int32_t *table, const int32_t *lengths,
                               const CacheData &c, uint16_t *O, float *lse, void *ws, hipStream_t st)
 {
-    float *parts = static_cast<float *>(ws);
-    if (g.D == 64) return g.e4m3 ? launch_decode<64, true>(g, Q, table, lengths, c, O, lse, parts, st)
-                                 : launch_decode<64, false>(g, Q, table, lengths, c, O, lse, parts, st);
-    return g.e4m3 ? launch_decode<128, true>(g, Q, table, lengths, c, O, lse, parts, st)
-                  : launch_decode<128, false>(g, Q, table, lengths, c, O, lse, parts, st);
+    if (g.D == 64) return g.e4m3 ? launch_decode<64, true>(g, Q, table, lengths, c, O, lse, ws, st)
+                                 : launch_decode<64, false>(g, Q, table, lengths, c, O, lse, ws, st);
+    return g.e4m3 ? launch_decode<128, true>(g, Q, table, lengths, c, O, lse, ws, st)
+                  : launch_decode<128, false>(g, Q, table, lengths, c, O, lse, ws, st);
 }
 
 }  // namespace adaspark

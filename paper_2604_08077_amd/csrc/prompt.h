@@ -66,25 +66,6 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptGeom &g, int s)
     return p;
 }
 
-__device__ __forceinline__ PromptSeq seq_uniform(const PromptSeq &p)
-{
-    return {__builtin_amdgcn_readfirstlane(p.q0), __builtin_amdgcn_readfirstlane(p.n), __builtin_amdgcn_readfirstlane(p.k0),
-            __builtin_amdgcn_readfirstlane(p.m)};
-}
-
-// Inclusive scan over a wavefront's lanes, without LDS: within rows of 16, then each row's sum carried on.
-__device__ __forceinline__ int wave_scan(int x)
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-    return x;
-}
-__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
-
 // What a workgroup does follows from lengths that only the device knows, so every wavefront finds its own work: the w-th block of
 // all.  A wavefront's lanes hold the lengths of 512 sequences, eight each; beyond, sequences are taken 512 at a time.
 // count(n, m, t): blocks of a sequence (n queries, m keys) with a walk of at least t tiles (t = 0: all of them); they are the
@@ -290,19 +271,22 @@ __device__ __forceinline__ bool part_row(const PromptGeom &g, const PromptCut &c
     const int tok = (int)(row / g.Hq), a = (int)(row - (long long)tok * g.Hq);
     r.row = row;
     r.kv = a / g.G;
-    int lo = 0, hi = g.B;  // the last sequence with a start at or before the token
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (g.q_start[mid] <= tok) lo = mid;
-        else hi = mid;
+    // the last sequence with a start at or before the token: 64 of them at a time
+    const int lane = threadIdx.x & 63;
+    int lo = 0;
+    for (int s = 0; s < g.B; s += 64) {
+        const unsigned long long b = __ballot(s + lane < g.B && g.q_start[min(s + lane, g.B - 1)] <= tok);
+        if (b == 0ull) break;
+        lo = s + 63 - __clzll(b);
+        if (b != ~0ull) break;
     }
     r.seq = lo;
-    const PromptSeq p = prompt_seq(g, lo);
-    if (tok < p.q0 || tok >= p.q0 + p.n) return false;
-    const int x = (tok - p.q0) * g.G + (a - r.kv * g.G), i = x / R;
+    const int q0 = min(max(g.q_start[lo], 0), g.Tq), end = min(max(g.q_start[lo + 1], q0), g.Tq);
+    if (tok < q0 || tok >= end) return false;
+    const int x = (tok - q0) * g.G + (a - r.kv * g.G), i = x / R;
     r.at = x - i * R;
-    const size_t id = (size_t)r.kv * cut.blocks + row_block_id(g, R, lo, p.q0, i);
-    const int lane = threadIdx.x & 63, item = parts.item[id * PARTS_MAX + lane];
+    const size_t id = (size_t)r.kv * cut.blocks + row_block_id(g, R, lo, q0, i);
+    const int item = parts.item[id * PARTS_MAX + lane];
     r.n = min(parts.count[id], PARTS_MAX);
     if (r.n <= 1) return false;
     r.item = lane < r.n ? min(max(item, 0), cut.cap - 1) : 0;  // (starts that overlap leave blocks that nobody worked)

@@ -120,7 +120,7 @@ static PromptBwdWorkspace bwd_workspace_of(const PromptGeom &g, int D, void *ws)
 size_t prompt_bwd_workspace_bytes(const PromptGeom &g, int D) { return bwd_workspace_of(g, D, nullptr).bytes; }
 
 // Start values of every row: 256 / (D / 8) rows to a workgroup, D / 8 lanes to a row.  A row without keys (log-sum-exp -inf) gets
-// no part in anything.  The first B * Hkv workgroups leave the mean keys, a thread to a column and as many keys as there are threads for;
+// no part in anything.  The first B * Hkv workgroups leave the mean keys, a thread to a column of some of the keys;
 // the very first wavefront also the length of a span.
 template <int D>
 __global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most, int *__restrict__ span, const uint16_t *__restrict__ K,
@@ -140,8 +140,18 @@ __global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most
         const PromptSeq p = prompt_seq(g, s);
         const int n = min(p.m, 64);
         float x = 0.f;
-        for (int i = threadIdx.x / D; i < n; i += 256 / D)  // 64 keys, evenly spread
-            x += __uint_as_float((uint32_t)K[(size_t)(p.k0 + (int)((long long)i * p.m / n)) * g.ks + (size_t)kv * D + d] << 16);
+        const uint16_t *k = K + (size_t)p.k0 * g.ks + (size_t)kv * D + d;
+        if (n > 0) {
+            uint32_t v[64 * D / 256];  // 64 keys (all of them, some twice, where there are fewer), evenly spread
+#pragma unroll
+            for (int u = 0; u < 64 * D / 256; ++u) {
+                const int i = (int)threadIdx.x / D + u * (256 / D);
+                v[u] = k[(long long)(n == 64 ? (int)(((long long)i * p.m) >> 6) : min(i, n - 1)) * g.ks];
+            }
+#pragma unroll
+            for (int u = 0; u < 64 * D / 256; ++u)
+                if ((int)threadIdx.x / D + u * (256 / D) < n) x += __uint_as_float(v[u] << 16);
+        }
         sums[threadIdx.x] = x;
         __syncthreads();
         if (threadIdx.x < D) {

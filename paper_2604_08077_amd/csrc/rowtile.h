@@ -30,6 +30,19 @@ inline unsigned head_grid(int Hkv, int per_head)
     return (unsigned)per_head * (unsigned)Hkv;
 }
 
+// Inclusive scan over a wavefront's lanes, without LDS: within rows of 16, then each row's sum carried on.
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
+
 // Direct-to-LDS copies with an address per lane: lane l moves the 16 (4) bytes at src to lds_addr + 16 * l (4 * l).
 __device__ __forceinline__ void dma_lane16(uint32_t lds_addr, const void *src)
 {
