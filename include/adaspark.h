@@ -422,7 +422,7 @@ int adaspark_prompt_attn_bwd(const adaspark_prompts *prompts, const void *Q, con
  * the OCP format), with a scale per token and KV head, fp32 [pages][kv_heads][page_size]: the row's largest magnitude / 448 (at least 2^-126; 0
  * for a row of zeros); a code is the nearest value of the format to x / scale, and stands for code * scale.  A row that holds an
  * infinity or a NaN has a NaN for its scale.
- * Limits: page_size a power of two; table_pages*page_size <= 2^30; pages*page_size < 2^31; q_heads, kv_heads, head_dim as above,
+ * Limits: page_size a power of two; table_pages*page_size <= 2^30; pages*page_size and page_size*kv_heads*head_dim < 2^31; q_heads, kv_heads, head_dim as above,
  * sequences*q_heads < 2^31 (the sequences of a decode step that share a KV head's keys with more than 16 query heads read them once per 16).
  */
 typedef enum {

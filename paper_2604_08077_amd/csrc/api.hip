@@ -99,6 +99,7 @@ int check_cache(const adaspark_cache *c)
     if (rc != ADASPARK_OK) return rc;
     if ((c->page_size & (c->page_size - 1)) != 0) return ADASPARK_EUNSUPPORTED;
     if ((long long)c->table_pages * c->page_size > (1ll << 30) || (long long)c->pages * c->page_size >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
+    if ((long long)c->kv_heads * c->head_dim >= (1 << 24) || (long long)c->kv_heads * c->head_dim * c->page_size >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
     if ((long long)c->sequences * c->q_heads >= (1ll << 31) || c->q_heads >= (1 << 16)) return ADASPARK_EUNSUPPORTED;
     return ADASPARK_OK;
 }

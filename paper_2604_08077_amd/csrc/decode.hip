@@ -20,23 +20,26 @@ namespace adaspark {
 
 typedef int s32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int DECODE_WAVES = 2;
+// In 8 bits a tile takes twice the instructions a byte (codes to bf16), so tiles are half as large and twice as many wavefronts work.
+constexpr int decode_tile(bool e4m3) { return e4m3 ? 4096 : 8192; }  // bytes of keys in a tile, and of values
+constexpr int decode_waves(bool e4m3) { return e4m3 ? 4 : 2; }
 constexpr int DECODE_PLAN_SEQS = 512;  // sequences that a wavefront's lanes hold the lengths of, eight each
 constexpr int DECODE_PLACES = 512;    // workgroups that the chip holds at once, two to a CU
 
 template <int D, bool E4M3>
 struct Decode {
-    static constexpr int WAVES = DECODE_WAVES;
+    static constexpr int WAVES = decode_waves(E4M3);
+    static constexpr int TILE = decode_tile(E4M3);
     static constexpr int THREADS = 64 * WAVES;
     static constexpr int ROW = D * (E4M3 ? 1 : 2);  // bytes of a key
-    static constexpr int KEYS = 8192 / ROW;         // of a tile: 32, 64 or 128
+    static constexpr int KEYS = TILE / ROW;         // of a tile: 32 or 64
     static constexpr int CPR = ROW / 16;            // 16-byte chunks of a row
     static constexpr int RPI = 64 / CPR;            // rows of one direct-to-LDS instruction
-    static constexpr int NI = 8;                    // such instructions for 8 KB
-    static constexpr int OFF_V = 8192;
-    static constexpr int OFF_KS = 16384;            // scales of the keys, then of the values
-    static constexpr int STAGE = 16384 + (E4M3 ? 2 * KEYS * 4 : 0);
-    static constexpr int PAGES = (KEYS < 64 ? 64 : KEYS) * 4;  // the page of each key of a tile
+    static constexpr int NI = TILE / 1024;          // such instructions for a tile's keys
+    static constexpr int OFF_V = TILE;
+    static constexpr int OFF_KS = 2 * TILE;         // 64 scales of keys, then of values
+    static constexpr int STAGE = 2 * TILE + (E4M3 ? 512 : 0);
+    static constexpr int PAGES = 256;               // the page of each key of a tile (of 32 keys: twice)
     static constexpr int WAVE_BYTES = 2 * STAGE + 2 * PAGES;
     static constexpr int BYTES = WAVES * WAVE_BYTES;
     static_assert(BYTES <= 80 * 1024, "half the LDS of a CU");
@@ -50,7 +53,10 @@ struct DecodePart {
     int item0;           // number of the sequence's first part
     int key0, key1;
 };
-__host__ __device__ inline int decode_unit(const CacheGeom &g) { return 2 * DECODE_WAVES * 8192 / (g.D * (g.e4m3 ? 1 : 2)); }  // keys
+__host__ __device__ inline int decode_unit(const CacheGeom &g)  // keys of two tiles for each wavefront
+{
+    return 2 * decode_waves(g.e4m3) * decode_tile(g.e4m3) / (g.D * (g.e4m3 ? 1 : 2));
+}
 
 // Parts that a KV head and 16 query heads of its group get: a workgroup each, whole rounds of the chip, at least two for
 // a sequence on average -- the parts have one length, and lengths differ.
@@ -169,7 +175,7 @@ __host__ __device__ inline size_t decode_part_floats(int D) { return 16 * (size_
 __host__ __device__ inline size_t decode_plan_bytes(const CacheGeom &g) { return ((size_t)g.B * 8 + 255) & ~(size_t)255; }
 
 template <int D, bool E4M3>
-__global__ __launch_bounds__(64 * DECODE_WAVES) void decode_attn_kernel(CacheGeom g, const uint16_t *__restrict__ Q,
+__global__ __launch_bounds__(64 * decode_waves(E4M3), 2) void decode_attn_kernel(CacheGeom g, const uint16_t *__restrict__ Q,
                                                           const int32_t *__restrict__ table,
                                                           const int32_t *__restrict__ lengths,
                                                           const unsigned char *__restrict__ Kc,
@@ -205,37 +211,37 @@ __global__ __launch_bounds__(64 * DECODE_WAVES) void decode_attn_kernel(CacheGeo
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem + (uint32_t)(wave * C::WAVE_BYTES));
     const uint32_t pages0 = lds0 + 2 * C::STAGE;
     const int32_t *trow = table + (size_t)p.s * g.table_pages;
-    const int in_page = (1 << g.shift) - 1;
+    const int in_page = (1 << g.shift) - 1, head_row = kv << g.shift;
+    const uint32_t page_bytes = (uint32_t)(g.Hkv << g.shift) * (uint32_t)C::ROW;  // (below 2^32: the entry points check)
     // the table entries of a tile's keys (past the sequence's end: its last key's)
     auto ask_pages = [&](int t, int buf) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < C::PAGES / 256; ++u) {
-            const int key = min(p.key0 + t * KEYS + ((u * 64 + lane) & (KEYS - 1)), p.key1 - 1);
-            dma_lane4(__builtin_amdgcn_readfirstlane(pages0 + (uint32_t)(buf * C::PAGES + u * 256)), trow + (key >> g.shift));
-        }
+        const int key = min(p.key0 + t * KEYS + (lane & (KEYS - 1)), p.key1 - 1);
+        dma_256_s(__builtin_amdgcn_readfirstlane(pages0 + (uint32_t)(buf * C::PAGES)), uniform_ptr(trow), 4u * (uint32_t)(key >> g.shift));
     };
     // a tile's rows (keys of no page are read from page 0, and zeroed before they are used)
     auto ask_rows = [&](int t, int buf) __attribute__((always_inline)) {
         const uint32_t st = lds0 + (uint32_t)(buf * C::STAGE);
-        auto place = [&](int r) -> size_t {
-            const int key = min(p.key0 + t * KEYS + r, p.key1 - 1);
-            const int page = lds_read<int>(pages0 + (uint32_t)(buf * C::PAGES + 4 * r));
-            return (((size_t)((unsigned)page < (unsigned)g.pages ? page : 0) * g.Hkv + kv) << g.shift) + (key & in_page);
+        auto row_of = [&](int r, int &page) __attribute__((always_inline)) -> uint32_t {  // the row in its page's run
+            page = lds_read<int>(pages0 + (uint32_t)(buf * C::PAGES + 4 * r));
+            page = (unsigned)page < (unsigned)g.pages ? page : 0;
+            return (uint32_t)((min(p.key0 + t * KEYS + r, p.key1 - 1) & in_page) + head_row);
         };
 #pragma unroll
         for (int u = 0; u < C::NI; ++u) {
             const int r = u * C::RPI + lane / C::CPR;
-            const size_t off = place(r) * C::ROW + decode_chunk_at<C::ROW>(r, lane & 15) * 16;
+            int page;
+            const uint32_t row = row_of(r, page);
+            const unsigned long long off = (unsigned long long)(unsigned)page * page_bytes +
+                                           (row * (uint32_t)C::ROW + (uint32_t)decode_chunk_at<C::ROW>(r, lane & 15) * 16u);
             dma_lane16(__builtin_amdgcn_readfirstlane(st + (uint32_t)(u * 1024)), Kc + off);
             dma_lane16(__builtin_amdgcn_readfirstlane(st + (uint32_t)(C::OFF_V + u * 1024)), Vc + off);
         }
         if (E4M3) {
-#pragma unroll
-            for (int u = 0; u < KEYS / 64; ++u) {
-                const size_t off = place(u * 64 + lane);
-                dma_lane4(__builtin_amdgcn_readfirstlane(st + (uint32_t)(C::OFF_KS + u * 256)), ks + off);
-                dma_lane4(__builtin_amdgcn_readfirstlane(st + (uint32_t)(C::OFF_KS + KEYS * 4 + u * 256)), vs + off);
-            }
+            int page;
+            const uint32_t row = row_of(lane & (KEYS - 1), page);
+            const unsigned long long off = (unsigned long long)(unsigned)page * (page_bytes / C::ROW) + row;
+            dma_lane4(__builtin_amdgcn_readfirstlane(st + (uint32_t)C::OFF_KS), ks + off);
+            dma_lane4(__builtin_amdgcn_readfirstlane(st + (uint32_t)(C::OFF_KS + 256)), vs + off);
         }
     };
     auto wait_all = []() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
@@ -257,15 +263,9 @@ __global__ __launch_bounds__(64 * DECODE_WAVES) void decode_attn_kernel(CacheGeo
         wait_all();  // this tile's rows and the next one's pages are there, and nobody reads the other stage any more
         const int next = t + C::WAVES;
         // Which of this tile's keys there are, before their table entries make room for those of the tile after the next.
-        bool whole = true;
-        unsigned long long there[(KEYS + 63) / 64];
-#pragma unroll
-        for (int u = 0; u < (KEYS + 63) / 64; ++u) {
-            const int r = u * 64 + (lane & (KEYS - 1));
-            const int page = lds_read<int>(pages0 + (uint32_t)(buf * C::PAGES + 4 * r));
-            there[u] = __ballot(p.key0 + t * KEYS + r < p.key1 && (unsigned)page < (unsigned)g.pages);
-            whole = whole && there[u] == ~0ull;
-        }
+        const int mine = lane & (KEYS - 1), mypage = lds_read<int>(pages0 + (uint32_t)(buf * C::PAGES + 4 * mine));
+        const unsigned long long there = __ballot(p.key0 + t * KEYS + mine < p.key1 && (unsigned)mypage < (unsigned)g.pages);
+        const bool whole = there == ~0ull;
         if (next < ntiles) {
             if (next + C::WAVES < ntiles) ask_pages(next + C::WAVES, buf);
             ask_rows(next, buf ^ 1);
@@ -273,12 +273,12 @@ __global__ __launch_bounds__(64 * DECODE_WAVES) void decode_attn_kernel(CacheGeo
         const uint32_t st = lds0 + (uint32_t)(buf * C::STAGE);
         if (!whole) {  // rows that are not there: values (and their scales) of zero, so that a probability of zero adds nothing
             for (int r = 0; r < KEYS; ++r)
-                if (!((there[r >> 6] >> (r & 63)) & 1ull)) {
+                if (!((there >> r) & 1ull)) {
                     if (lane < C::CPR)
                         *reinterpret_cast<__attribute__((address_space(3))) u32x4 *>(st + C::OFF_V + decode_off<C::ROW>(r, lane)) =
                             u32x4{0u, 0u, 0u, 0u};
                     if (E4M3 && lane == 0)
-                        *reinterpret_cast<__attribute__((address_space(3))) float *>(st + C::OFF_KS + KEYS * 4 + 4 * r) = 0.f;
+                        *reinterpret_cast<__attribute__((address_space(3))) float *>(st + C::OFF_KS + 256 + 4 * r) = 0.f;
                 }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
@@ -308,7 +308,7 @@ __global__ __launch_bounds__(64 * DECODE_WAVES) void decode_attn_kernel(CacheGeo
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
                     const int r = 16 * kg + 4 * q4 + v;
-                    if (!((there[kg >> 2] >> (r & 63)) & 1ull)) sacc[kg][v] = -INFINITY;
+                    if (!((there >> r) & 1ull)) sacc[kg][v] = -INFINITY;
                 }
         }
         float mx = -INFINITY;
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(64 * DECODE_WAVES) void decode_attn_kernel(CacheGeo
                 w[v] = __builtin_amdgcn_exp2f(fmaf(sacc[kg][v], c2, -m_sub));
                 l_run += w[v];
             }
-            if (E4M3) w *= lds_read<f32x4>(st + (uint32_t)(C::OFF_KS + KEYS * 4 + 4 * (16 * kg + 4 * q4)));
+            if (E4M3) w *= lds_read<f32x4>(st + (uint32_t)(C::OFF_KS + 256 + 4 * (16 * kg + 4 * q4)));
             // P.V takes bf16 operands: a weight is off by up to 2^-8 of itself, as in the other attention kernels
 #pragma unroll
             for (int v = 0; v < 4; ++v) pf[kg >> 1][4 * (kg & 1) + v] = (__bf16)w[v];
