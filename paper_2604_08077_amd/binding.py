@@ -9,8 +9,8 @@ from __future__ import annotations
 
 import ctypes
 import os
-from contextlib import nullcontext
 from dataclasses import dataclass
+from functools import lru_cache
 from typing import NamedTuple
 
 import torch
@@ -554,51 +554,75 @@ def cube_select_shared(shape: Shape, Q: torch.Tensor, kbar: torch.Tensor, top_p:
 
 
 # ---- packed prompts and the paged cache.  These calls run on the device of their tensors, whichever is the current one, on
-# torch's current stream of that device.
+# torch's current stream of that device.  They are short -- a decode step takes the GPU some ten microseconds --, so what only depends on
+# a shape's values (the C struct, the size of a workspace) is worked out once for each shape.
 
 
-def _same_device(first: torch.Tensor, *others):
-    """A context with the tensors' device as the current one; raises if they are not all on it."""
-    if not isinstance(first, torch.Tensor) or first.device.type != "cuda":
-        raise ValueError("expected GPU tensors (this package has no CPU path)")
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"tensors on different devices: {first.device} and {t.device}")
-    return nullcontext() if first.device.index == torch.cuda.current_device() else torch.cuda.device(first.device)
-
-
-def _rows(t: torch.Tensor, tokens: int, heads: int, head_dim: int, name: str) -> tuple[int, int]:
-    """(pointer, stride of a token) of a bf16 [tokens, heads, head_dim] whose tokens may lie apart."""
+def _device(t: torch.Tensor, name: str) -> int:
     if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
         raise ValueError(f"{name} must be a GPU tensor (this package has no CPU path)")
-    if t.dtype != torch.bfloat16 or tuple(t.shape) != (tokens, heads, head_dim):
+    return t.get_device()
+
+
+def _at(t, dev: int, dtype, numel: int, name: str) -> int:
+    """Pointer of a contiguous tensor of that type and size on device ``dev``."""
+    if isinstance(t, torch.Tensor) and t.get_device() == dev and t.dtype == dtype and t.numel() == numel and t.is_contiguous():
+        return t.data_ptr()
+    _dev(t, dtype, numel, name)  # says what is wrong, unless it is the device
+    raise ValueError(f"{name} is on another device: cuda:{t.get_device()}, expected cuda:{dev}")
+
+
+def _rows_at(t, dev: int, tokens: int, heads: int, head_dim: int, name: str) -> tuple[int, int]:
+    """(pointer, stride of a token or 0) of a bf16 [tokens, heads, head_dim] whose tokens may lie apart."""
+    if _device(t, name) != dev:
+        raise ValueError(f"{name} is on another device: cuda:{t.get_device()}, expected cuda:{dev}")
+    if t.dtype != torch.bfloat16 or t.shape != (tokens, heads, head_dim):
         raise ValueError(f"{name}: expected torch.bfloat16 {(tokens, heads, head_dim)}, got {t.dtype} {tuple(t.shape)}")
-    row = heads * head_dim
-    if tokens == 0 or t.is_contiguous():
+    if t.is_contiguous() or tokens == 0:
         return t.data_ptr(), 0
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim) or (tokens > 1 and t.stride(0) < row):
+    step, head, one = t.stride()
+    if one != 1 or (heads > 1 and head != head_dim) or (tokens > 1 and step < heads * head_dim):
         raise ValueError(f"{name}: the heads of a token have to lie one behind the other, got strides {t.stride()}")
-    return t.data_ptr(), t.stride(0) if tokens > 1 else 0
+    return t.data_ptr(), step if tokens > 1 else 0
 
 
-def _optional(t, dtype, numel, name):
-    return None if t is None else _dev(t, dtype, numel, name)
+def _run(dev: int, fn_name: str, *args) -> None:
+    """The call on device ``dev``, on torch's current stream there."""
+    fn = getattr(load(), fn_name)
+    if dev == torch.cuda.current_device():
+        status = fn(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, torch.cuda.current_stream().cuda_stream)
+    if status != 0:
+        raise AdasparkError(status, fn_name)
 
 
-def prompt_workspace_bytes(shape: PromptShape, which_call: int, causal: bool = True) -> int:
-    n, cs = ctypes.c_size_t(0), shape._c()
-    _check(load().adaspark_prompt_workspace_bytes(ctypes.byref(cs), which_call, int(bool(causal)), ctypes.byref(n)),
-           "adaspark_prompt_workspace_bytes")
-    return n.value
-
-
-def _scratch(need: int, workspace, like: torch.Tensor):
-    """(keeps it alive, pointer, bytes) of the caller's workspace, or of one made here."""
+def _scratch(need: int, workspace, like: torch.Tensor, dev: int):
+    """(workspace, pointer, bytes): the caller's, or one made here."""
     if workspace is None:
         if need == 0:
             return None, None, 0
         workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
-    return workspace, _dev(workspace, torch.uint8, workspace.numel(), "workspace"), workspace.numel()
+    return workspace, _at(workspace, dev, torch.uint8, workspace.numel(), "workspace"), workspace.numel()
+
+
+@lru_cache(maxsize=256)
+def _prompts_c(shape: PromptShape, q_stride: int, k_stride: int, v_stride: int):
+    return ctypes.byref(shape._c(q_stride, k_stride, v_stride))
+
+
+@lru_cache(maxsize=256)
+def _cache_c(shape: CacheShape):
+    return ctypes.byref(shape._c())
+
+
+@lru_cache(maxsize=256)
+def prompt_workspace_bytes(shape: PromptShape, which_call: int, causal: bool = True) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().adaspark_prompt_workspace_bytes(_prompts_c(shape, 0, 0, 0), which_call, int(bool(causal)), ctypes.byref(n)),
+           "adaspark_prompt_workspace_bytes")
+    return n.value
 
 
 def prompt_attn(shape: PromptShape, Q, K, V, q_start, k_start=None, causal: bool = True, O=None, lse=None, workspace=None,
@@ -609,38 +633,36 @@ def prompt_attn(shape: PromptShape, Q, K, V, q_start, k_start=None, causal: bool
     lse that belong to no sequence are left as they were."""
     k_start = q_start if k_start is None else k_start
     Tq, Tk, Hq, Hkv, D, n = shape.q_tokens, shape.k_tokens, shape.q_heads, shape.kv_heads, shape.head_dim, shape.sequences
-    q, k, v = _rows(Q, Tq, Hq, D, "Q"), _rows(K, Tk, Hkv, D, "K"), _rows(V, Tk, Hkv, D, "V")
-    with _same_device(Q, K, V, q_start, k_start, O, lse, workspace):
-        if O is None:
-            O = torch.empty((Tq, Hq, D), dtype=torch.bfloat16, device=Q.device)
-        if lse is None and return_lse:
-            lse = torch.empty((Tq, Hq), dtype=torch.float32, device=Q.device)
-        cs = shape._c(q[1], k[1], v[1])
-        ws, ws_ptr, ws_bytes = _scratch(prompt_workspace_bytes(shape, PROMPT_ATTN, causal), workspace, Q)
-        _check(load().adaspark_prompt_attn(
-            ctypes.byref(cs), q[0], k[0], v[0], _dev(q_start, torch.int32, n + 1, "q_start"),
-            _dev(k_start, torch.int32, n + 1, "k_start"), int(bool(causal)), _dev(O, torch.bfloat16, Tq * Hq * D, "O"),
-            _optional(lse, torch.float32, Tq * Hq, "lse"), ws_ptr, ws_bytes, _stream()), "adaspark_prompt_attn")
+    dev = _device(Q, "Q")
+    q, k, v = _rows_at(Q, dev, Tq, Hq, D, "Q"), _rows_at(K, dev, Tk, Hkv, D, "K"), _rows_at(V, dev, Tk, Hkv, D, "V")
+    if O is None:
+        O = torch.empty((Tq, Hq, D), dtype=torch.bfloat16, device=Q.device)
+    if lse is None and return_lse:
+        lse = torch.empty((Tq, Hq), dtype=torch.float32, device=Q.device)
+    ws, ws_ptr, ws_bytes = _scratch(prompt_workspace_bytes(shape, PROMPT_ATTN, causal), workspace, Q, dev)
+    _run(dev, "adaspark_prompt_attn", _prompts_c(shape, q[1], k[1], v[1]), q[0], k[0], v[0],
+         _at(q_start, dev, torch.int32, n + 1, "q_start"), _at(k_start, dev, torch.int32, n + 1, "k_start"), int(bool(causal)),
+         _at(O, dev, torch.bfloat16, Tq * Hq * D, "O"), None if lse is None else _at(lse, dev, torch.float32, Tq * Hq, "lse"),
+         ws_ptr, ws_bytes)
     return (O, lse) if return_lse else O
 
 
 def prompt_attn_bwd(shape: PromptShape, Q, K, V, O, lse, dO, q_start, k_start=None, causal: bool = True, workspace=None,
                     dQ=None, dK=None, dV=None):
-    """Backward of ``prompt_attn`` -> (dQ, dK, dV) bf16, contiguous."""
+    """Backward of ``prompt_attn`` -> (dQ, dK, dV) bf16, contiguous.  Rows that belong to no sequence are left as they were."""
     k_start = q_start if k_start is None else k_start
     Tq, Tk, Hq, Hkv, D, n = shape.q_tokens, shape.k_tokens, shape.q_heads, shape.kv_heads, shape.head_dim, shape.sequences
-    q, k, v = _rows(Q, Tq, Hq, D, "Q"), _rows(K, Tk, Hkv, D, "K"), _rows(V, Tk, Hkv, D, "V")
-    with _same_device(Q, K, V, O, lse, dO, q_start, k_start, workspace, dQ, dK, dV):
-        new = lambda t, *size: torch.empty(size, dtype=torch.bfloat16, device=Q.device) if t is None else t  # noqa: E731
-        dQ, dK, dV = new(dQ, Tq, Hq, D), new(dK, Tk, Hkv, D), new(dV, Tk, Hkv, D)
-        cs = shape._c(q[1], k[1], v[1])
-        ws, ws_ptr, ws_bytes = _scratch(prompt_workspace_bytes(shape, PROMPT_ATTN_BWD, causal), workspace, Q)
-        _check(load().adaspark_prompt_attn_bwd(
-            ctypes.byref(cs), q[0], k[0], v[0], _dev(O, torch.bfloat16, Tq * Hq * D, "O"),
-            _dev(lse, torch.float32, Tq * Hq, "lse"), _dev(dO, torch.bfloat16, Tq * Hq * D, "dO"),
-            _dev(q_start, torch.int32, n + 1, "q_start"), _dev(k_start, torch.int32, n + 1, "k_start"), int(bool(causal)),
-            _dev(dQ, torch.bfloat16, Tq * Hq * D, "dQ"), _dev(dK, torch.bfloat16, Tk * Hkv * D, "dK"),
-            _dev(dV, torch.bfloat16, Tk * Hkv * D, "dV"), ws_ptr, ws_bytes, _stream()), "adaspark_prompt_attn_bwd")
+    dev, bf16 = _device(Q, "Q"), torch.bfloat16
+    q, k, v = _rows_at(Q, dev, Tq, Hq, D, "Q"), _rows_at(K, dev, Tk, Hkv, D, "K"), _rows_at(V, dev, Tk, Hkv, D, "V")
+    dQ = torch.empty((Tq, Hq, D), dtype=bf16, device=Q.device) if dQ is None else dQ
+    dK = torch.empty((Tk, Hkv, D), dtype=bf16, device=Q.device) if dK is None else dK
+    dV = torch.empty((Tk, Hkv, D), dtype=bf16, device=Q.device) if dV is None else dV
+    ws, ws_ptr, ws_bytes = _scratch(prompt_workspace_bytes(shape, PROMPT_ATTN_BWD, causal), workspace, Q, dev)
+    _run(dev, "adaspark_prompt_attn_bwd", _prompts_c(shape, q[1], k[1], v[1]), q[0], k[0], v[0], _at(O, dev, bf16, Tq * Hq * D, "O"),
+         _at(lse, dev, torch.float32, Tq * Hq, "lse"), _at(dO, dev, bf16, Tq * Hq * D, "dO"),
+         _at(q_start, dev, torch.int32, n + 1, "q_start"), _at(k_start, dev, torch.int32, n + 1, "k_start"), int(bool(causal)),
+         _at(dQ, dev, bf16, Tq * Hq * D, "dQ"), _at(dK, dev, bf16, Tk * Hkv * D, "dK"), _at(dV, dev, bf16, Tk * Hkv * D, "dV"),
+         ws_ptr, ws_bytes)
     return dQ, dK, dV
 
 
@@ -653,75 +675,70 @@ def alloc_cache(shape: CacheShape, device="cuda") -> Cache:
     return Cache(*codes, *(torch.zeros(size[:3], dtype=torch.float32, device=device) for _ in range(2)))
 
 
-def _cache_args(shape: CacheShape, cache: Cache, table) -> tuple:
-    """Pointers of the cache's buffers and of the page table."""
-    if shape.format not in CACHE_FORMATS:
-        raise ValueError(f"format: expected one of {tuple(CACHE_FORMATS)}, got {shape.format!r}")
+def _cache_at(shape: CacheShape, cache: Cache, table, dev: int) -> tuple:
+    """Pointers of the cache's buffers, and of the page table."""
     tokens = shape.pages * shape.kv_heads * shape.page_size
     if shape.format == "bf16":
         if cache.k_scale is not None or cache.v_scale is not None:
             raise ValueError("a bf16 cache has no scales")
-        held = [_dev(t, torch.bfloat16, tokens * shape.head_dim, n) for t, n in ((cache.K, "cache.K"), (cache.V, "cache.V"))] + [None, None]
+        held = (_at(cache.K, dev, torch.bfloat16, tokens * shape.head_dim, "cache.K"),
+                _at(cache.V, dev, torch.bfloat16, tokens * shape.head_dim, "cache.V"), None, None)
+    elif shape.format == "e4m3":
+        kind = lambda t: torch.uint8 if isinstance(t, torch.Tensor) and t.dtype == torch.uint8 else torch.float8_e4m3fn  # noqa: E731
+        held = (_at(cache.K, dev, kind(cache.K), tokens * shape.head_dim, "cache.K"),
+                _at(cache.V, dev, kind(cache.V), tokens * shape.head_dim, "cache.V"),
+                _at(cache.k_scale, dev, torch.float32, tokens, "cache.k_scale"),
+                _at(cache.v_scale, dev, torch.float32, tokens, "cache.v_scale"))
     else:
-        held = [_dev(t, torch.uint8 if isinstance(t, torch.Tensor) and t.dtype == torch.uint8 else torch.float8_e4m3fn,
-                     tokens * shape.head_dim, n) for t, n in ((cache.K, "cache.K"), (cache.V, "cache.V"))]
-        held += [_dev(cache.k_scale, torch.float32, tokens, "cache.k_scale"), _dev(cache.v_scale, torch.float32, tokens, "cache.v_scale")]
-    return held, _dev(table, torch.int32, shape.sequences * shape.table_pages, "table")
+        raise ValueError(f"format: expected one of {tuple(CACHE_FORMATS)}, got {shape.format!r}")
+    return held, _at(table, dev, torch.int32, shape.sequences * shape.table_pages, "table")
 
 
 def cache_write(shape: CacheShape, K, V, start, cache: Cache, table, lengths) -> None:
     """The new tokens K, V (bf16 [tokens, Hkv, D], packed by start, int32 [sequences + 1]) take the last positions of their sequences:
     lengths (int32 [sequences]) counts them already.  table int32 [sequences, table_pages]: the sequences' pages, -1 for none."""
-    tokens = K.shape[0]
-    k, v = _rows(K, tokens, shape.kv_heads, shape.head_dim, "K"), _rows(V, tokens, shape.kv_heads, shape.head_dim, "V")
-    with _same_device(K, V, start, table, lengths, *cache):
-        held, pages = _cache_args(shape, cache, table)
-        cs = shape._c()
-        _check(load().adaspark_cache_write(
-            ctypes.byref(cs), tokens, k[0], k[1], v[0], v[1], _dev(start, torch.int32, shape.sequences + 1, "start"), pages,
-            _dev(lengths, torch.int32, shape.sequences, "lengths"), *held, _stream()), "adaspark_cache_write")
+    dev, tokens = _device(K, "K"), K.shape[0]
+    k = _rows_at(K, dev, tokens, shape.kv_heads, shape.head_dim, "K")
+    v = _rows_at(V, dev, tokens, shape.kv_heads, shape.head_dim, "V")
+    held, pages = _cache_at(shape, cache, table, dev)
+    _run(dev, "adaspark_cache_write", _cache_c(shape), tokens, k[0], k[1], v[0], v[1],
+         _at(start, dev, torch.int32, shape.sequences + 1, "start"), pages,
+         _at(lengths, dev, torch.int32, shape.sequences, "lengths"), *held)
 
 
 def cache_read(shape: CacheShape, cache: Cache, table, start, tokens: int, K=None, V=None):
     """Histories read back -> (K, V) bf16 [tokens, Hkv, D]: rows start[s] .. start[s+1] are the positions 0, 1, ... of sequence s.
     With start as k_start they feed ``prompt_attn``."""
-    size = (tokens, shape.kv_heads, shape.head_dim)
-    with _same_device(cache.K, cache.V, cache.k_scale, cache.v_scale, table, start, K, V):
-        held, pages = _cache_args(shape, cache, table)
-        if K is None:
-            K = torch.empty(size, dtype=torch.bfloat16, device=cache.K.device)
-        if V is None:
-            V = torch.empty(size, dtype=torch.bfloat16, device=cache.K.device)
-        n = tokens * shape.kv_heads * shape.head_dim
-        cs = shape._c()
-        _check(load().adaspark_cache_read(
-            ctypes.byref(cs), tokens, _dev(start, torch.int32, shape.sequences + 1, "start"), pages, *held,
-            _dev(K, torch.bfloat16, n, "K"), _dev(V, torch.bfloat16, n, "V"), _stream()), "adaspark_cache_read")
+    dev, size = _device(cache.K, "cache.K"), (tokens, shape.kv_heads, shape.head_dim)
+    held, pages = _cache_at(shape, cache, table, dev)
+    K = torch.empty(size, dtype=torch.bfloat16, device=cache.K.device) if K is None else K
+    V = torch.empty(size, dtype=torch.bfloat16, device=cache.K.device) if V is None else V
+    n = tokens * shape.kv_heads * shape.head_dim
+    _run(dev, "adaspark_cache_read", _cache_c(shape), tokens, _at(start, dev, torch.int32, shape.sequences + 1, "start"), pages, *held,
+         _at(K, dev, torch.bfloat16, n, "K"), _at(V, dev, torch.bfloat16, n, "V"))
     return K, V
 
 
+@lru_cache(maxsize=256)
 def decode_workspace_bytes(shape: CacheShape) -> int:
-    n, cs = ctypes.c_size_t(0), shape._c()
-    _check(load().adaspark_decode_workspace_bytes(ctypes.byref(cs), ctypes.byref(n)), "adaspark_decode_workspace_bytes")
+    n = ctypes.c_size_t(0)
+    _check(load().adaspark_decode_workspace_bytes(_cache_c(shape), ctypes.byref(n)), "adaspark_decode_workspace_bytes")
     return n.value
 
 
 def decode_attn(shape: CacheShape, Q, cache: Cache, table, lengths, O=None, lse=None, workspace=None, return_lse: bool = False):
     """Attention of one new token of each sequence (Q bf16 [sequences, Hq, D]) over its first lengths[s] positions of the cache ->
     O bf16 [sequences, Hq, D] (and lse fp32 [sequences, Hq])."""
-    rows, D = shape.sequences * shape.q_heads, shape.head_dim
-    with _same_device(Q, table, lengths, O, lse, workspace, *cache):
-        held, pages = _cache_args(shape, cache, table)
-        if O is None:
-            O = torch.empty((shape.sequences, shape.q_heads, D), dtype=torch.bfloat16, device=Q.device)
-        if lse is None and return_lse:
-            lse = torch.empty((shape.sequences, shape.q_heads), dtype=torch.float32, device=Q.device)
-        ws, ws_ptr, ws_bytes = _scratch(decode_workspace_bytes(shape), workspace, Q)
-        cs = shape._c()
-        _check(load().adaspark_decode_attn(
-            ctypes.byref(cs), _dev(Q, torch.bfloat16, rows * D, "Q"), pages, _dev(lengths, torch.int32, shape.sequences, "lengths"),
-            *held, _dev(O, torch.bfloat16, rows * D, "O"), _optional(lse, torch.float32, rows, "lse"), ws_ptr, ws_bytes,
-            _stream()), "adaspark_decode_attn")
+    rows, D, dev = shape.sequences * shape.q_heads, shape.head_dim, _device(Q, "Q")
+    held, pages = _cache_at(shape, cache, table, dev)
+    if O is None:
+        O = torch.empty((shape.sequences, shape.q_heads, D), dtype=torch.bfloat16, device=Q.device)
+    if lse is None and return_lse:
+        lse = torch.empty((shape.sequences, shape.q_heads), dtype=torch.float32, device=Q.device)
+    ws, ws_ptr, ws_bytes = _scratch(decode_workspace_bytes(shape), workspace, Q, dev)
+    _run(dev, "adaspark_decode_attn", _cache_c(shape), _at(Q, dev, torch.bfloat16, rows * D, "Q"), pages,
+         _at(lengths, dev, torch.int32, shape.sequences, "lengths"), *held, _at(O, dev, torch.bfloat16, rows * D, "O"),
+         None if lse is None else _at(lse, dev, torch.float32, rows, "lse"), ws_ptr, ws_bytes)
     return (O, lse) if return_lse else O
 
 
