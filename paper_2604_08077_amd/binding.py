@@ -587,13 +587,14 @@ def _rows_at(t, dev: int, tokens: int, heads: int, head_dim: int, name: str) -> 
 
 
 def _run(dev: int, fn_name: str, *args) -> None:
-    """The call on device ``dev``, on torch's current stream there."""
+    """The call on device ``dev``, on torch's current stream there (as a plain handle: torch.cuda.current_stream makes an object
+    of it, a quarter of a short call's time on the host)."""
     fn = getattr(load(), fn_name)
     if dev == torch.cuda.current_device():
-        status = fn(*args, torch.cuda.current_stream().cuda_stream)
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     else:
         with torch.cuda.device(dev):
-            status = fn(*args, torch.cuda.current_stream().cuda_stream)
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     if status != 0:
         raise AdasparkError(status, fn_name)
 

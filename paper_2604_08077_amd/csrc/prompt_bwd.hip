@@ -4,9 +4,9 @@
 // with dK, dV summed over the G heads of a KV head's group.  p is rebuilt from the log-sum-exp.  As in the backward of the cube-selective
 // attention (attn_bwd.hip) two kernels, one that keeps rows and one that keeps keys, do it without atomics: seven products
 // where five would do with them, and the same bits every time.
-//   prompt_dq_kernel   128 rows of a (sequence, KV head), 32 to a wavefront with Q and dO in registers, over tiles of 64 keys:
+//   prompt_dq    128 rows of a (sequence, KV head), 32 to a wavefront with Q and dO in registers, over tiles of 64 keys:
 //                      S^T = K.Q^T, dP^T = V.dO^T, dQ^T += K^T.dS^T.
-//   prompt_dkv_kernel  128 keys, 32 to a wavefront with K and V in registers, over tiles of 64 rows:
+//   prompt_dkv   128 keys, 32 to a wavefront with K and V in registers, over tiles of 64 rows:
 //                      S = Q.K^T, dP = dO.V^T, dV^T += dO^T.P, dK^T += Q^T.dS.
 // All tiles are rows as the caller holds them, read in LDS both ways (rowtile.h).  The accumulators of S start from
 // -lse * sqrt(D) and those of dP from -delta, which prompt_prep_kernel leaves per row.
@@ -18,7 +18,7 @@
 // against 64 bits, keys of as much common as own direction, goes from 4.0e-3 to 2.6e-3.
 //
 // Where few key blocks have long walks, a walk is cut into spans, a workgroup each, which leave fp32 sums in the
-// workspace; prompt_reduce_kernel adds them in their order.  Walks of few row blocks are shared out as in the forward (prompt.h).
+// workspace; prompt_bwd_join_kernel adds them in their order.  Walks of few row blocks are shared out as in the forward (prompt.h).
 //
 // Workgroups of four wavefronts and two stages, two to a CU, which are not in step (a training pass over 16k tokens in 5 sequences of 28/4 heads
 // of 128, in ms, with eight wavefronts and three stages 2.31, so 2.20).
@@ -177,13 +177,21 @@ __global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most
     }
 }
 
+struct PromptBwdArgs {
+    const uint16_t *Q, *K, *V, *dO;
+    const float *lse2, *delta, *mean;
+    const int *span;
+    float *part;
+    uint16_t *dQ, *dK, *dV;
+};
+
 template <int D, bool SPLIT>
-__global__ __launch_bounds__(PB_THREADS, 2) void prompt_dq_kernel(PromptGeom g, PromptCut cut, PromptParts parts,
-                                                                  const uint16_t *__restrict__ Q, const uint16_t *__restrict__ K,
-                                                                  const uint16_t *__restrict__ V, const uint16_t *__restrict__ dO,
-                                                                  const float *__restrict__ lse2p, const float *__restrict__ deltap,
-                                                                  const float *__restrict__ mean, uint16_t *__restrict__ dQ)
+__device__ __forceinline__ void prompt_dq(const PromptGeom &g, const PromptCut &cut, const PromptParts &parts, unsigned block,
+                                          const PromptBwdArgs &arg)
 {
+    const uint16_t *__restrict__ Q = arg.Q, *__restrict__ K = arg.K, *__restrict__ V = arg.V, *__restrict__ dO = arg.dO;
+    const float *__restrict__ lse2p = arg.lse2, *__restrict__ deltap = arg.delta, *__restrict__ mean = arg.mean;
+    uint16_t *__restrict__ dQ = arg.dQ;
     using C = PromptBwd<D>;
     constexpr int NS = 2, KSTEPS = D / 32, DT = D / 16;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
@@ -191,7 +199,7 @@ __global__ __launch_bounds__(PB_THREADS, 2) void prompt_dq_kernel(PromptGeom g, 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
     int kv, slot;
-    if (!head_slot(blockIdx.x, g.Hkv, SPLIT ? cut.cap : (int)cut.blocks, kv, slot)) return;
+    if (!head_slot((int)block, g.Hkv, SPLIT ? cut.cap : (int)cut.blocks, kv, slot)) return;
     PromptItem it;
     if constexpr (SPLIT) it = prompt_item<PB_BLOCK>(g, slot, cut.cap);
     else it = {longest_first(g, slot, (g.Tk + KEY_TILE - 1) / KEY_TILE,
@@ -374,13 +382,13 @@ __global__ __launch_bounds__(PB_THREADS, 2) void prompt_dq_kernel(PromptGeom g, 
 
 // The parts of a row's dQ added in their order, a wavefront for each (token, query head): lane l has D / 64 columns.
 template <int D>
-__global__ __launch_bounds__(256) void prompt_dq_join_kernel(PromptGeom g, PromptCut cut, PromptParts parts, const float *__restrict__ mean,
-                                                             uint16_t *__restrict__ dQ)
+__device__ __forceinline__ void join_dq(const PromptGeom &g, const PromptCut &cut, const PromptParts &parts, unsigned block,
+                                        const float *__restrict__ mean, uint16_t *__restrict__ dQ)
 {
     constexpr int N = D / 64;
     const int lane = threadIdx.x & 63;
     PartRow r;
-    if (!part_row(g, cut, parts, PB_BLOCK, (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r)) return;
+    if (!part_row(g, cut, parts, PB_BLOCK, (long long)block * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r)) return;
     const float *from = parts.result + (size_t)r.kv * cut.cap * dq_part_floats(D);
     float o[N], total = 0.f;
 #pragma unroll
@@ -421,13 +429,13 @@ __device__ __forceinline__ int key_blocks(const PromptGeom &g, int n, int m, int
 }
 
 template <int D>
-__global__ __launch_bounds__(PB_THREADS, 2) void prompt_dkv_kernel(PromptGeom g, int per_head, PromptSpans cut,
-                                                                const int *__restrict__ span_p, const uint16_t *__restrict__ Q, const uint16_t *__restrict__ K,
-                                                                const uint16_t *__restrict__ V, const uint16_t *__restrict__ dO,
-                                                                const float *__restrict__ lse2p, const float *__restrict__ deltap,
-                                                                float *__restrict__ partial, uint16_t *__restrict__ dK,
-                                                                uint16_t *__restrict__ dV)
+__device__ __forceinline__ void prompt_dkv(const PromptGeom &g, int per_head, const PromptSpans &cut, unsigned block, const PromptBwdArgs &arg)
 {
+    const uint16_t *__restrict__ Q = arg.Q, *__restrict__ K = arg.K, *__restrict__ V = arg.V, *__restrict__ dO = arg.dO;
+    const float *__restrict__ lse2p = arg.lse2, *__restrict__ deltap = arg.delta;
+    const int *__restrict__ span_p = arg.span;
+    float *__restrict__ partial = arg.part;
+    uint16_t *__restrict__ dK = arg.dK, *__restrict__ dV = arg.dV;
     using C = PromptBwd<D>;
     constexpr int NS = 2, KSTEPS = D / 32, DT = D / 16, PER = C::PER, CPR = C::CPR;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
@@ -435,7 +443,7 @@ __global__ __launch_bounds__(PB_THREADS, 2) void prompt_dkv_kernel(PromptGeom g,
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
     int kv, slot;
-    if (!head_slot(blockIdx.x, g.Hkv, per_head, kv, slot)) return;
+    if (!head_slot((int)block, g.Hkv, per_head, kv, slot)) return;
     // Later spans first (only long blocks have them), and the first span of all blocks last: the launch ends with its shortest items.  And
     // an XCD gets every so many-th block, not every so many-th span.
     const int nb = (int)cut.blocks, span = cut.most - 1 - slot / nb, span_len = *span_p;
@@ -636,76 +644,109 @@ __global__ __launch_bounds__(PB_THREADS, 2) void prompt_dkv_kernel(PromptGeom g,
     }
 }
 
-// The spans' sums of a key block, added in their order: four workgroups to a block, one for each wavefront's keys; NS * DT * 64
-// places in MFMA output order.
-template <int D>
-__global__ __launch_bounds__(256) void prompt_reduce_kernel(PromptGeom g, PromptSpans cut, const int *__restrict__ span_p, const float *__restrict__ partial,
-                                                            uint16_t *__restrict__ dK, uint16_t *__restrict__ dV)
+// The products of one launch: key blocks' workgroups first, then row blocks' -- the two are independent, and the end of one's work is
+// filled with the other's (a training pass over 2k tokens in 3 sequences of 8/2 heads of 64, us, as two launches 80, so 61).
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(PB_THREADS, 2) void prompt_bwd_kernel(PromptGeom g, PromptSpans spans, unsigned key_grid, PromptCut cut,
+                                                                   PromptParts parts, PromptBwdArgs arg)
 {
-    constexpr int NS = 2, DT = D / 16;
-    const int wave = blockIdx.x % PB_WAVES, kv = (int)(blockIdx.x / PB_WAVES % (unsigned)g.Hkv), id = (int)(blockIdx.x / PB_WAVES / (unsigned)g.Hkv);
-    int lo = 0, hi = g.B;  // the sequence of block `id`: the last one whose blocks begin at or before it
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (key_block_id(mid, prompt_seq(g, mid).k0, 0) <= id) lo = mid;
-        else hi = mid;
+    if (blockIdx.x < key_grid) prompt_dkv<D>(g, (int)spans.blocks * spans.most, spans, blockIdx.x, arg);
+    else prompt_dq<D, SPLIT>(g, cut, parts, blockIdx.x - key_grid, arg);
+}
+
+// The spans' sums of a key block, added in their order: a workgroup for 256 of the 16 D * 8 places (four values each, in MFMA
+// output order) that the block's dV and its dK have.
+constexpr int reduce_groups(int D) { return PB_BLOCK * D / 4 / 256; }
+template <int D>
+__device__ __forceinline__ void reduce_spans(const PromptGeom &g, const PromptSpans &cut, unsigned block, int span_len,
+                                             const float *__restrict__ partial, uint16_t *__restrict__ dK, uint16_t *__restrict__ dV)
+{
+    constexpr int NS = 2, DT = D / 16, GROUPS = reduce_groups(D), SUM = PB_BLOCK * D / 4;
+    const int kv = (int)(block / GROUPS % (unsigned)g.Hkv), id = (int)(block / GROUPS / (unsigned)g.Hkv), lane = threadIdx.x & 63;
+    // the sequence of block `id`: the last one whose blocks begin at or before it
+    int lo = 0;
+    for (int s = 0; s < g.B; s += 64) {
+        const int at = min(s + lane, g.B - 1);
+        const unsigned long long b = __ballot(s + lane < g.B && key_block_id(at, min(max(g.k_start[at], 0), g.Tk), 0) <= id);
+        if (b == 0ull) break;
+        lo = s + 63 - __clzll(b);
+        if (b != ~0ull) break;
     }
     const PromptSeq p = prompt_seq(g, lo);
     const int j = id - key_block_id(lo, p.k0, 0);
     if (j < 0 || j * (long long)PB_BLOCK >= p.m) return;
     const long long rows = (long long)p.n * g.G, first = g.causal ? min(rows, max(0ll, (long long)j * PB_BLOCK - (p.m - p.n)) * g.G) : 0;
-    const int span_len = *span_p, all = (int)((rows - first + 63) / 64), spans = (all + span_len - 1) / span_len;
+    const int all = (int)((rows - first + 63) / 64), spans = (all + span_len - 1) / span_len;
     if (spans <= 1) return;
-    const f32x4 *from = reinterpret_cast<const f32x4 *>(partial) + ((size_t)kv * cut.blocks + id) * cut.most * (2 * PB_BLOCK * D / 4) + wave * (NS * DT * 64);
-    const float c = 1.0f / sqrtf((float)D);
-    for (int x = threadIdx.x; x < NS * DT * 64; x += 256) {
-        f32x4 v = {0.f, 0.f, 0.f, 0.f}, k = v;
-#pragma unroll 2
-        for (int i = 0; i < spans; ++i) {
-            v += from[(size_t)i * (2 * PB_BLOCK * D / 4) + x];
-            k += from[(size_t)i * (2 * PB_BLOCK * D / 4) + PB_BLOCK * D / 4 + x];
+    const int x = (int)(block % GROUPS) * 256 + threadIdx.x;
+    const f32x4 *from = reinterpret_cast<const f32x4 *>(partial) + ((size_t)kv * cut.blocks + id) * cut.most * (2 * SUM) + x;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f}, k = v;
+    for (int i = 0; i < spans; i += 4) {  // four spans' loads at a time
+        f32x4 y[4][2];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const f32x4 *at = from + (size_t)min(i + u, spans - 1) * (2 * SUM);
+            y[u][0] = at[0];
+            y[u][1] = at[SUM];
         }
-        const int lane = x & 63, e = (x >> 6) % DT, s = (x >> 6) / DT, key = j * PB_BLOCK + 32 * wave + 16 * s + (lane & 15);
-        if (key >= p.m) continue;
-        const size_t o = ((size_t)(p.k0 + key) * g.Hkv + kv) * D + 16 * e + 4 * (lane >> 4);
-        *reinterpret_cast<uint2 *>(dV + o) = pack_bf16(v);
-        *reinterpret_cast<uint2 *>(dK + o) = pack_bf16(k * c);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + u < spans) {
+                v += y[u][0];
+                k += y[u][1];
+            }
     }
+    const int wave = x / (NS * DT * 64), e = (x >> 6) % DT, s = (x >> 6) / DT % NS, key = j * PB_BLOCK + 32 * wave + 16 * s + (lane & 15);
+    if (key >= p.m) return;
+    const size_t o = ((size_t)(p.k0 + key) * g.Hkv + kv) * D + 16 * e + 4 * (lane >> 4);
+    *reinterpret_cast<uint2 *>(dV + o) = pack_bf16(v);
+    *reinterpret_cast<uint2 *>(dK + o) = pack_bf16(k * (1.0f / sqrtf((float)D)));
+}
+
+// What is left where walks were cut: key blocks' spans, then rows' parts.
+template <int D>
+__global__ __launch_bounds__(256) void prompt_bwd_join_kernel(PromptGeom g, PromptSpans spans, unsigned key_groups, PromptCut cut,
+                                                              PromptParts parts, PromptBwdArgs arg)
+{
+    if (blockIdx.x < key_groups) reduce_spans<D>(g, spans, blockIdx.x, *arg.span, arg.part, arg.dK, arg.dV);
+    else join_dq<D>(g, cut, parts, blockIdx.x - key_groups, arg.mean, arg.dQ);
+}
+
+template <int D, bool SPLIT>
+static hipError_t launch_products(const PromptGeom &g, const PromptSpans &spans, unsigned key_grid, const PromptCut &cut,
+                                  const PromptParts &parts, const PromptBwdArgs &arg, hipStream_t st)
+{
+    using C = PromptBwd<D>;
+    static LdsOptIn opted;  // one per kernel instantiation
+    const hipError_t e = opted.ensure(reinterpret_cast<const void *>(&prompt_bwd_kernel<D, SPLIT>), C::BYTES);
+    if (e != hipSuccess) return e;
+    const unsigned row_grid = g.Tq > 0 ? head_grid(g.Hkv, SPLIT ? cut.cap : (int)cut.blocks) : 0u;
+    hipLaunchKernelGGL((prompt_bwd_kernel<D, SPLIT>), dim3(key_grid + row_grid), dim3(PB_THREADS), C::BYTES, st, g, spans, key_grid, cut, parts, arg);
+    return hipGetLastError();
 }
 
 template <int D>
 static hipError_t launch_bwd(const PromptGeom &g, const uint16_t *Q, const uint16_t *K, const uint16_t *V, const uint16_t *O,
                              const float *lse, const uint16_t *dO, uint16_t *dQ, uint16_t *dK, uint16_t *dV, void *ws, hipStream_t st)
 {
-    using C = PromptBwd<D>;
     const PromptBwdWorkspace w = bwd_workspace_of(g, D, ws);
-    const PromptSpans cut = prompt_spans(g);
-    static LdsOptIn opted_q, opted_parts, opted_kv;
-    hipError_t e = opted_q.ensure(reinterpret_cast<const void *>(&prompt_dq_kernel<D, false>), C::BYTES);
-    if (e == hipSuccess) e = opted_parts.ensure(reinterpret_cast<const void *>(&prompt_dq_kernel<D, true>), C::BYTES);
-    if (e == hipSuccess) e = opted_kv.ensure(reinterpret_cast<const void *>(&prompt_dkv_kernel<D>), C::BYTES);
-    if (e != hipSuccess) return e;
+    const PromptSpans spans = prompt_spans(g);
+    const PromptCut cut = prompt_cut(g, PB_BLOCK);
+    const PromptBwdArgs arg{Q, K, V, dO, w.lse2, w.delta, w.mean, w.span, w.part, dQ, dK, dV};
     const long long rows = (long long)g.Tq * g.Hq, per = 256 / (D / 8);
     hipLaunchKernelGGL((prompt_prep_kernel<D>), dim3((unsigned)((long long)g.B * g.Hkv + (rows + 1 + per - 1) / per)), dim3(256), 0, st, g,
-                       cut.most, w.span, K, w.mean, rows, O, dO, lse, w.lse2, w.delta);
-    if (g.Tk > 0) {
-        const int keys = (int)cut.blocks * cut.most;
-        hipLaunchKernelGGL((prompt_dkv_kernel<D>), dim3(head_grid(g.Hkv, keys)), dim3(PB_THREADS), C::BYTES, st, g, keys, cut, w.span, Q, K, V, dO,
-                           w.lse2, w.delta, w.part, dK, dV);
-        if (cut.most > 1)
-            hipLaunchKernelGGL((prompt_reduce_kernel<D>), dim3((unsigned)(cut.blocks * g.Hkv * PB_WAVES)), dim3(256), 0, st, g, cut, w.span, w.part, dK, dV);
-    }
-    if (g.Tq > 0) {
-        const PromptCut rc = prompt_cut(g, PB_BLOCK);
-        if (rc.cap == 0) {
-            hipLaunchKernelGGL((prompt_dq_kernel<D, false>), dim3(head_grid(g.Hkv, (int)rc.blocks)), dim3(PB_THREADS), C::BYTES, st, g, rc, w.rows, Q,
-                               K, V, dO, w.lse2, w.delta, w.mean, dQ);
-        } else {
-            hipLaunchKernelGGL((prompt_dq_kernel<D, true>), dim3(head_grid(g.Hkv, rc.cap)), dim3(PB_THREADS), C::BYTES, st, g, rc, w.rows, Q, K, V,
-                               dO, w.lse2, w.delta, w.mean, dQ);
-            hipLaunchKernelGGL((prompt_dq_join_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, g, rc, w.rows, w.mean, dQ);
-        }
-    }
+                       spans.most, w.span, K, w.mean, rows, O, dO, lse, w.lse2, w.delta);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    // (a multiple of 8: the row blocks' workgroups keep their XCDs)
+    const unsigned key_grid = g.Tk > 0 ? (head_grid(g.Hkv, (int)spans.blocks * spans.most) + 7) / 8 * 8 : 0u;
+    e = cut.cap == 0 ? launch_products<D, false>(g, spans, key_grid, cut, w.rows, arg, st)
+                     : launch_products<D, true>(g, spans, key_grid, cut, w.rows, arg, st);
+    if (e != hipSuccess) return e;
+    const unsigned key_groups = g.Tk > 0 && spans.most > 1 ? (unsigned)(spans.blocks * g.Hkv * reduce_groups(D)) : 0u;
+    const unsigned row_groups = cut.cap > 0 ? (unsigned)((rows + 3) / 4) : 0u;
+    if (key_groups + row_groups > 0)
+        hipLaunchKernelGGL((prompt_bwd_join_kernel<D>), dim3(key_groups + row_groups), dim3(256), 0, st, g, spans, key_groups, cut, w.rows, arg);
     return hipGetLastError();
 }
 
