@@ -83,8 +83,9 @@ __device__ __forceinline__ PromptLengths prompt_lengths(const PromptGeom &g, int
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int c = 0; c < PROMPT_CHUNKS; ++c) {
+        if (c >= l.chunks) break;  // (nothing beyond is looked at)
         PromptSeq p = {0, 0, 0, 0};
-        if (c < l.chunks && s0 + 64 * c + lane < g.B) p = prompt_seq(g, s0 + 64 * c + lane);
+        if (s0 + 64 * c + lane < g.B) p = prompt_seq(g, s0 + 64 * c + lane);
         l.q0[c] = p.q0;
         l.n[c] = p.n;
         l.k0[c] = p.k0;
@@ -102,8 +103,10 @@ __device__ __forceinline__ int blocks_from(const PromptLengths &l, int t, Count 
 {
     int x = 0;
 #pragma unroll
-    for (int c = 0; c < PROMPT_CHUNKS; ++c)
-        if (c < l.chunks) x += count(l.n[c], l.m[c], t);
+    for (int c = 0; c < PROMPT_CHUNKS; ++c) {
+        if (c >= l.chunks) break;
+        x += count(l.n[c], l.m[c], t);
+    }
     return wave_total(x);
 }
 // The r-th of the blocks with a walk of t0 .. t1 - 1 tiles (t1 < 0: or more).
@@ -113,7 +116,7 @@ __device__ __forceinline__ PromptBlock nth_block(const PromptLengths &l, int r, 
     PromptBlock b = {{0, 0, 0, 0}, -1, 0};
 #pragma unroll
     for (int c = 0; c < PROMPT_CHUNKS; ++c) {
-        if (c >= l.chunks || b.seq >= 0) continue;
+        if (c >= l.chunks) break;
         const int longer = t1 < 0 ? 0 : count(l.n[c], l.m[c], t1), mine = count(l.n[c], l.m[c], t0) - longer, incl = wave_scan(mine);
         const unsigned long long hit = __ballot(r < incl);
         if (hit != 0ull) {
@@ -122,6 +125,7 @@ __device__ __forceinline__ PromptBlock nth_block(const PromptLengths &l, int r, 
             b.block = __builtin_amdgcn_readlane(longer, src) + r - __builtin_amdgcn_readlane(incl - mine, src);
             b.p = {__builtin_amdgcn_readlane(l.q0[c], src), __builtin_amdgcn_readlane(l.n[c], src), __builtin_amdgcn_readlane(l.k0[c], src),
                    __builtin_amdgcn_readlane(l.m[c], src)};
+            break;
         }
         r -= __builtin_amdgcn_readlane(incl, 63);
     }
@@ -137,8 +141,8 @@ __device__ __forceinline__ int walk_level(int b)  // the b-th length
 template <typename Count>
 __device__ __forceinline__ PromptBlock longest_first(const PromptGeom &g, int w, int most_tiles, Count count)
 {
-    int top = 1;
-    while (walk_level(top) <= most_tiles) ++top;  // (no block is that long)
+    // (no block is as long as level `top`, the one behind that of most_tiles)
+    const int log = 31 - __clz(most_tiles | 1), top = most_tiles < 2 ? most_tiles + 1 : 2 * log + ((most_tiles >> (log - 1)) & 1) + 1;
     for (int s0 = 0; s0 < g.B; s0 += PROMPT_SEQS) {
         const PromptLengths l = prompt_lengths(g, s0);
         const int all = blocks_from(l, 0, count);
@@ -161,7 +165,7 @@ __device__ __forceinline__ PromptBlock longest_first(const PromptGeom &g, int w,
 template <int R>
 __device__ __forceinline__ int row_blocks(int n, int m, int G, int causal, int t)
 {
-    const int nb = (int)(((long long)n * G + R - 1) / R);
+    const int nb = (n * G - 1) / R + (n > 0 ? 1 : 0);
     if (t == 0) return nb;
     const int keys = 64 * (t - 1);  // a walk of t tiles needs more than so many
     if (!causal) return m > keys ? nb : 0;

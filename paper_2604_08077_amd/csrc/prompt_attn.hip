@@ -89,24 +89,6 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptGeom g, Promp
         mine = min(max(mine - first, 0), ntiles);
     }
 
-    // the wavefront's rows (past the last one it is repeated)
-    int reach[NS];
-    bool valid[NS];
-    size_t rid[NS];
-    bf16x8 qf[NS][KSTEPS];
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-        const int row = row0 + 32 * wave + 16 * s + n16, r = min(row, rows - 1), tok = token_of_row(g, r);
-        valid[s] = row < rows;
-        reach[s] = reach_of(r);
-        const int head = kv * g.G + (r - tok * g.G);
-        rid[s] = (size_t)(p.q0 + tok) * g.Hq + head;
-        const uint16_t *q = Q + (size_t)(p.q0 + tok) * g.qs + (size_t)head * D + 8 * q4;
-#pragma unroll
-        for (int c = 0; c < KSTEPS; ++c) qf[s][c] = *reinterpret_cast<const bf16x8 *>(q + 32 * c);
-    }
-    const int reach_lo = __builtin_amdgcn_readfirstlane(reach[0]);  // of the wavefront's first row: no other reaches less far
-
     // Loads: piece u of this wavefront is RPI rows of a tile, a 16-byte slot to a lane, which fetches the chunk that belongs there.
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem);
     const uint32_t piece0 = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)(wave * C::DMA * 1024));
@@ -138,6 +120,29 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptGeom g, Promp
     };
     auto issue_k = [&](int t, int st) __attribute__((always_inline)) { issue(khead, g.ks, kofs, t, st * C::TILE); };
     auto issue_v = [&](int t, int st) __attribute__((always_inline)) { issue(vhead, g.vs, vofs, t, C::OFF_V + st * C::TILE); };
+
+    if (ntiles > 0) {
+        issue_k(0, 0);
+        issue_v(0, 0);
+    }
+
+    // the wavefront's rows (past the last one it is repeated)
+    int reach[NS];
+    bool valid[NS];
+    size_t rid[NS];
+    bf16x8 qf[NS][KSTEPS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int row = row0 + 32 * wave + 16 * s + n16, r = min(row, rows - 1), tok = token_of_row(g, r);
+        valid[s] = row < rows;
+        reach[s] = reach_of(r);
+        const int head = kv * g.G + (r - tok * g.G);
+        rid[s] = (size_t)(p.q0 + tok) * g.Hq + head;
+        const uint16_t *q = Q + (size_t)(p.q0 + tok) * g.qs + (size_t)head * D + 8 * q4;
+#pragma unroll
+        for (int c = 0; c < KSTEPS; ++c) qf[s][c] = *reinterpret_cast<const bf16x8 *>(q + 32 * c);
+    }
+    const int reach_lo = __builtin_amdgcn_readfirstlane(reach[0]);  // of the wavefront's first row: no other reaches less far
 
     const float c2 = 1.44269504088896340736f / sqrtf((float)D);  // softmax scale in base 2
     float m_run[NS], l_run[NS];  // reference point of the exponentials; sum of the lane's keys' weights
@@ -278,10 +283,6 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptGeom g, Promp
         for (int s = 0; s < NS; ++s) l_run[s] += sum[s];
     };
 
-    if (ntiles > 0) {
-        issue_k(0, 0);
-        issue_v(0, 0);
-    }
     // One slot a tile: the products P.V of tile t-1 and S of tile t, then the softmax of tile t.
     const std::true_type yes;
     const std::false_type no;
