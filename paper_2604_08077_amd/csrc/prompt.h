@@ -5,6 +5,8 @@
 // last key, so that a follow-up turn's queries attend the history before them.  A KV head's rows are numbered token by token,
 // row = token * G + head of the group: neighbouring rows reach equally far, and a token's G heads lie one behind the other in memory.
 #pragma once
+#include <algorithm>
+
 #include "rowtile.h"
 
 namespace adaspark {
@@ -184,19 +186,29 @@ __device__ __forceinline__ int row_block_id(const PromptGeom &g, int R, int s, i
 // Few blocks (a short turn on a long history, a handful of prompts): each block's walk over the keys is shared out to several
 // workgroups, a part each, and a second kernel puts a row's parts together.  A workgroup's item is (block, part); the parts of a block are
 // equally long, at most `chunk` tiles, and chunk follows from the lengths: as short as the number of items, `cap` a KV head, allows.
-constexpr int PART_MIN = 8;      // tiles: a part's result is written and read again, and a second launch made
-constexpr int PARTS_MAX = 64;    // of a block
-constexpr int PART_BLOCKS = 768; // blocks up to which walks are shared out: three to a place for a workgroup, 512 of which 256 CUs have
+constexpr int PART_MIN = 8;     // tiles
+constexpr int PARTS_MAX = 64;   // of a block
+constexpr int PART_PLACES = 512;  // workgroups that the chip holds at once, two to a CU
 struct PromptCut {
     int cap;           // items of a KV head at most; 0: walks are not shared out
     long long blocks;  // blocks of a KV head at most
 };
-inline PromptCut prompt_cut(const PromptGeom &g, int R)
+// Whether sharing out pays, from what a pass takes (us) either way: the longest walk, or all tiles over the places where that is more; shared
+// out, the tiles over the places, a second launch, and the parts' results written and read.  The lengths are on the device: sequences count as of one
+// length, the longest as twice that.  (Forward, not shared out and shared out: 4,096 tokens of 8/2 heads of 64 56, 49; 6,000 of 6/2 of 128 113, 85; 378
+// queries on 29k keys of 32/8 of 128 600, 122; but 2,000 of 28/4 of 128 49, 74; four prompts of 90 to 1,200 of 16/16 of 64 22, 34; 16,000 of 6/2 of
+// 128 374, 405.  The dQ kernel's line lies where this one does.)
+inline PromptCut prompt_cut(const PromptGeom &g, int R, int D)
 {
     PromptCut c = {0, row_block_bound(g, R)};
-    const long long blocks = c.blocks * g.Hkv;
-    if (g.B > PROMPT_SEQS || blocks > PART_BLOCKS || (g.Tk + KEY_TILE - 1) / KEY_TILE <= PART_MIN) return c;
-    c.cap = (int)((2 * blocks > 512 ? 2 * blocks : 512) / g.Hkv);
+    const double blocks = (double)c.blocks * g.Hkv, tile = D == 64 ? 1.0 : 1.3;
+    const double walk = ((double)g.Tk - (g.causal ? 0.5 * std::min(g.Tq, g.Tk) : 0.0)) / g.B / KEY_TILE + 0.5;  // of a block, on average
+    const double longest = (double)g.Tk / KEY_TILE * std::min(1.0, 2.0 / g.B), tiles = blocks * walk;
+    if (g.B > PROMPT_SEQS || longest <= PART_MIN) return c;
+    const double cap = std::max((double)PART_PLACES, 4 * blocks), part = std::max((double)PART_MIN, tiles / (cap - blocks));
+    const double busy = 1.25 * tiles / PART_PLACES;
+    const double results = 8.0 * D * g.Tq * g.Hq * (walk / part + 0.5);  // bytes, written and read at 4.5 TB/s
+    if (tile * std::max(part, busy) + 6 + results / 4.5e6 < tile * std::max(longest, busy)) c.cap = (int)(cap / g.Hkv);
     return c;
 }
 // What the second kernel goes by, in the workspace: for every block the number of its parts, and each part's item, whose number is

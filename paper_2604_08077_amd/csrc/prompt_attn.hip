@@ -364,7 +364,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g, PromptCu
 
 size_t prompt_workspace_bytes(const PromptGeom &g, int D)
 {
-    return prompt_parts(g, prompt_cut(g, PROMPT_ROWS), prompt_part_floats(D), nullptr).bytes;
+    return prompt_parts(g, prompt_cut(g, PROMPT_ROWS, D), prompt_part_floats(D), nullptr).bytes;
 }
 
 template <int D, bool SPLIT>
@@ -384,7 +384,7 @@ template <int D>
 static hipError_t launch_prompt_d(const PromptGeom &g, const uint16_t *Q, const uint16_t *K, const uint16_t *V, uint16_t *O, float *lse,
                                   void *ws, hipStream_t st)
 {
-    const PromptCut cut = prompt_cut(g, PROMPT_ROWS);
+    const PromptCut cut = prompt_cut(g, PROMPT_ROWS, D);
     const PromptParts parts = prompt_parts(g, cut, prompt_part_floats(D), ws);
     if (cut.cap == 0) return launch_walk<D, false>(g, cut, parts, Q, K, V, O, lse, st);
     const hipError_t e = launch_walk<D, true>(g, cut, parts, Q, K, V, O, lse, st);

@@ -109,7 +109,7 @@ static PromptBwdWorkspace bwd_workspace_of(const PromptGeom &g, int D, void *ws)
     p += 256;
     w.mean = reinterpret_cast<float *>(p);
     p += up((size_t)g.B * g.Hkv * D * 4);
-    w.rows = prompt_parts(g, prompt_cut(g, PB_BLOCK), dq_part_floats(D), p);
+    w.rows = prompt_parts(g, prompt_cut(g, PB_BLOCK, D), dq_part_floats(D), p);
     p += up(w.rows.bytes);
     w.lse2 = reinterpret_cast<float *>(p);
     w.delta = reinterpret_cast<float *>(p + rows);
@@ -731,7 +731,7 @@ static hipError_t launch_bwd(const PromptGeom &g, const uint16_t *Q, const uint1
 {
     const PromptBwdWorkspace w = bwd_workspace_of(g, D, ws);
     const PromptSpans spans = prompt_spans(g);
-    const PromptCut cut = prompt_cut(g, PB_BLOCK);
+    const PromptCut cut = prompt_cut(g, PB_BLOCK, D);
     const PromptBwdArgs arg{Q, K, V, dO, w.lse2, w.delta, w.mean, w.span, w.part, dQ, dK, dV};
     const long long rows = (long long)g.Tq * g.Hq, per = 256 / (D / 8);
     hipLaunchKernelGGL((prompt_prep_kernel<D>), dim3((unsigned)((long long)g.B * g.Hkv + (rows + 1 + per - 1) / per)), dim3(256), 0, st, g,
