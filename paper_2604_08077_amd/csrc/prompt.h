@@ -195,9 +195,9 @@ struct PromptCut {
 };
 // Whether sharing out pays, from what a pass takes (us) either way: the longest walk, or all tiles over the places where that is more; shared
 // out, the tiles over the places, a second launch, and the parts' results written and read.  The lengths are on the device: sequences count as of one
-// length, the longest as twice that.  (Forward, not shared out and shared out: 4,096 tokens of 8/2 heads of 64 56, 49; 6,000 of 6/2 of 128 113, 85; 378
-// queries on 29k keys of 32/8 of 128 600, 122; but 2,000 of 28/4 of 128 49, 74; four prompts of 90 to 1,200 of 16/16 of 64 22, 34; 16,000 of 6/2 of
-// 128 374, 405.  The dQ kernel's line lies where this one does.)
+// length, the longest as twice that.  (Forward, whole and shared out: 4,096 tokens of 8/2 heads of 64 58, 46; 6,000 of 6/2 of 128 114, 80; 378
+// queries on 29k keys of 32/8 of 128 600, 119; but 2,000 of 28/4 of 128 49, 66; four prompts of 90 to 1,200 of 16/16 of 64 22, 27; 16,000 of 6/2 of
+// 128 373, 393.  The backward pass, where dQ's walks are shared out by the same rule: 124, 98; 266, 232; 153, 168; 53, 55; 1,180, 1,240.)
 inline PromptCut prompt_cut(const PromptGeom &g, int R, int D)
 {
     PromptCut c = {0, row_block_bound(g, R)};
@@ -208,7 +208,7 @@ inline PromptCut prompt_cut(const PromptGeom &g, int R, int D)
     const double cap = std::max((double)PART_PLACES, 4 * blocks), part = std::max((double)PART_MIN, tiles / (cap - blocks));
     const double busy = 1.25 * tiles / PART_PLACES;
     const double results = 8.0 * D * g.Tq * g.Hq * (walk / part + 0.5);  // bytes, written and read at 4.5 TB/s
-    if (tile * std::max(part, busy) + 6 + results / 4.5e6 < tile * std::max(longest, busy)) c.cap = (int)(cap / g.Hkv);
+    if (tile * std::max(part, busy) + 8 + results / 4.5e6 < tile * std::max(longest, busy)) c.cap = (int)(cap / g.Hkv);
     return c;
 }
 // What the second kernel goes by, in the workspace: for every block the number of its parts, and each part's item, whose number is
@@ -275,38 +275,52 @@ __device__ __forceinline__ PromptItem prompt_item(const PromptGeom &g, int w, in
     return it;
 }
 
-// Row (token, query head) number `row` of Q, for a wavefront of the second kernel: its KV head, its place in its block, the block's parts;
-// lane i has the i-th part's item.  false: no sequence's, or a row whose one part wrote it.
+// A wavefront of the second kernel has up to four query heads of a token, 16 lanes to each: the lane's row, its KV head, its place in its
+// block, and the block's parts.  n == 0: no sequence's row, or one whose only part wrote it.
+constexpr int JOIN_HEADS = 4;
+inline unsigned join_groups(const PromptGeom &g) { return (unsigned)(((long long)g.Tq * ((g.Hq + JOIN_HEADS - 1) / JOIN_HEADS) + 3) / 4); }
 struct PartRow {
-    long long row;
-    int seq, kv, at, n, item;
+    size_t row;
+    int seq, kv, at, n, most;  // most: the largest n in the wavefront
+    const int *item;
 };
-__device__ __forceinline__ bool part_row(const PromptGeom &g, const PromptCut &cut, const PromptParts &parts, int R, long long row, PartRow &r)
+__device__ __forceinline__ PartRow part_row(const PromptGeom &g, const PromptCut &cut, const PromptParts &parts, int R, unsigned group)
 {
-    if (row >= (long long)g.Tq * g.Hq) return false;
-    const int tok = (int)(row / g.Hq), a = (int)(row - (long long)tok * g.Hq);
-    r.row = row;
-    r.kv = a / g.G;
+    PartRow r = {0, 0, 0, 0, 0, 0, parts.item};
+    const int lane = threadIdx.x & 63, per = (g.Hq + JOIN_HEADS - 1) / JOIN_HEADS;
+    const long long w = (long long)group * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int tok = (int)(w / per), a = (int)(w - (long long)tok * per) * JOIN_HEADS + (lane >> 4);
+    if (tok >= g.Tq) return r;
     // the last sequence with a start at or before the token: 64 of them at a time
-    const int lane = threadIdx.x & 63;
-    int lo = 0;
     for (int s = 0; s < g.B; s += 64) {
         const unsigned long long b = __ballot(s + lane < g.B && g.q_start[min(s + lane, g.B - 1)] <= tok);
         if (b == 0ull) break;
-        lo = s + 63 - __clzll(b);
+        r.seq = s + 63 - __clzll(b);
         if (b != ~0ull) break;
     }
-    r.seq = lo;
-    const int q0 = min(max(g.q_start[lo], 0), g.Tq), end = min(max(g.q_start[lo + 1], q0), g.Tq);
-    if (tok < q0 || tok >= end) return false;
-    const int x = (tok - q0) * g.G + (a - r.kv * g.G), i = x / R;
+    const int q0 = min(max(g.q_start[r.seq], 0), g.Tq), end = min(max(g.q_start[r.seq + 1], q0), g.Tq);
+    if (tok < q0 || tok >= end) return r;
+    const int head = min(a, g.Hq - 1);
+    r.row = (size_t)tok * g.Hq + head;
+    r.kv = head / g.G;
+    const int x = (tok - q0) * g.G + (head - r.kv * g.G), i = x / R;
     r.at = x - i * R;
-    const size_t id = (size_t)r.kv * cut.blocks + row_block_id(g, R, lo, q0, i);
-    const int item = parts.item[id * PARTS_MAX + lane];
-    r.n = min(parts.count[id], PARTS_MAX);
-    if (r.n <= 1) return false;
-    r.item = lane < r.n ? min(max(item, 0), cut.cap - 1) : 0;  // (starts that overlap leave blocks that nobody worked)
-    return true;
+    const size_t id = (size_t)r.kv * cut.blocks + row_block_id(g, R, r.seq, q0, i);
+    r.item += id * PARTS_MAX;
+    const int n = min(parts.count[id], PARTS_MAX);
+    r.n = a < g.Hq && n > 1 ? n : 0;
+    r.most = max(max(__builtin_amdgcn_readlane(r.n, 0), __builtin_amdgcn_readlane(r.n, 16)), max(__builtin_amdgcn_readlane(r.n, 32), __builtin_amdgcn_readlane(r.n, 48)));
+    return r;
+}
+// Where the results of parts x .. x + 3 of the lane's row lie, of `floats` each (past its last part the last one's again; starts that overlap
+// leave blocks that nobody worked: an item stays one of the KV head's).
+__device__ __forceinline__ void part_results(const PartRow &r, const PromptCut &cut, const PromptParts &parts, size_t floats, int x, const float *(&at)[4])
+{
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int item = min(max(r.item[max(min(x + u, r.n - 1), 0)], 0), cut.cap - 1);
+        at[u] = parts.result + ((size_t)r.kv * cut.cap + item) * floats;
+    }
 }
 
 size_t prompt_workspace_bytes(const PromptGeom &g, int D);

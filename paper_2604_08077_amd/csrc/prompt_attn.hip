@@ -322,44 +322,54 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptGeom g, Promp
     }
 }
 
-// The parts of a row put together, a wavefront for each (token, query head): lane l has D / 64 columns.
+// The parts of a row put together, four at a time.
 template <int D>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptGeom g, PromptCut cut, PromptParts parts, uint16_t *__restrict__ O,
                                                           float *__restrict__ lse)
 {
-    constexpr int N = D / 64;
-    const int lane = threadIdx.x & 63;
-    PartRow r;
-    if (!part_row(g, cut, parts, PROMPT_ROWS, (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r)) return;
-    const float *from = parts.result + (size_t)r.kv * cut.cap * prompt_part_floats(D);
-    const float2 ml = lane < r.n ? *reinterpret_cast<const float2 *>(from + r.item * prompt_part_floats(D) + PROMPT_ROWS * D + 2 * r.at)
-                                 : make_float2(-INFINITY, 0.f);
-    float M = ml.x;
+    constexpr int N = D / 16 / 4;  // groups of four columns that a lane has
+    const int sub = threadIdx.x & 15;
+    const PartRow r = part_row(g, cut, parts, PROMPT_ROWS, blockIdx.x);
+    float M = -INFINITY, L = 0.f;
+    f32x4 o[N];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
-    const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-    float L = w * ml.y, o[N];
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) L += __shfl_xor(L, d, 64);
-#pragma unroll
-    for (int k = 0; k < N; ++k) o[k] = 0.f;
-    for (int x = 0; x < r.n; x += 4) {  // four parts' loads at a time (past the last one it is read again, with a weight of 0)
-        float y[4][N];
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int k = 0; k < N; ++k) y[u][k] = from[__builtin_amdgcn_readlane(r.item, min(x + u, r.n - 1)) * prompt_part_floats(D) + r.at * D + N * lane + k];
+    for (int k = 0; k < N; ++k) o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < r.most; x += 4) {
+        const float *at[4];
+        part_results(r, cut, parts, prompt_part_floats(D), x, at);
+        float2 ml[4];
+        f32x4 y[4][N];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const float wx = x + u < r.n ? __shfl(w, x + u, 64) : 0.f;
+            ml[u] = *reinterpret_cast<const float2 *>(at[u] + PROMPT_ROWS * D + 2 * r.at);
 #pragma unroll
-            for (int k = 0; k < N; ++k) o[k] = fmaf(wx, y[u][k], o[k]);
+            for (int k = 0; k < N; ++k) y[u][k] = *reinterpret_cast<const f32x4 *>(at[u] + r.at * D + 4 * (N * sub + k));
+        }
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (x + u >= r.n) ml[u] = make_float2(-INFINITY, 0.f);
+            top = fmaxf(top, ml[u].x);
+        }
+        if (top == -INFINITY) continue;  // (no part so far has a key of the row)
+        const float keep = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - top);
+        M = top;
+        L *= keep;
+#pragma unroll
+        for (int k = 0; k < N; ++k) o[k] *= keep;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float w = ml[u].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[u].x - top);
+            L = fmaf(w, ml[u].y, L);
+#pragma unroll
+            for (int k = 0; k < N; ++k) o[k] += w * y[u][k];
         }
     }
+    if (r.n == 0) return;
     const float inv = M == -INFINITY ? 0.f : 1.0f / L;
 #pragma unroll
-    for (int k = 0; k < N; ++k) reinterpret_cast<__bf16 *>(O)[(size_t)r.row * D + N * lane + k] = (__bf16)(o[k] * inv);
-    if (lse != nullptr && lane == 0) lse[r.row] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * LN2;
+    for (int k = 0; k < N; ++k) *reinterpret_cast<uint2 *>(O + r.row * D + 4 * (N * sub + k)) = pack_bf16(o[k] * inv);
+    if (lse != nullptr && sub == 0) lse[r.row] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * LN2;
 }
 
 size_t prompt_workspace_bytes(const PromptGeom &g, int D)
@@ -389,7 +399,7 @@ static hipError_t launch_prompt_d(const PromptGeom &g, const uint16_t *Q, const 
     if (cut.cap == 0) return launch_walk<D, false>(g, cut, parts, Q, K, V, O, lse, st);
     const hipError_t e = launch_walk<D, true>(g, cut, parts, Q, K, V, O, lse, st);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((prompt_join_kernel<D>), dim3((unsigned)(((long long)g.Tq * g.Hq + 3) / 4)), dim3(256), 0, st, g, cut, parts, O, lse);
+    hipLaunchKernelGGL((prompt_join_kernel<D>), dim3(join_groups(g)), dim3(256), 0, st, g, cut, parts, O, lse);
     return hipGetLastError();
 }
 

@@ -380,40 +380,43 @@ __device__ __forceinline__ void prompt_dq(const PromptGeom &g, const PromptCut &
     }
 }
 
-// The parts of a row's dQ added in their order, a wavefront for each (token, query head): lane l has D / 64 columns.
+// The parts of a row's dQ added in their order, four at a time.
 template <int D>
-__device__ __forceinline__ void join_dq(const PromptGeom &g, const PromptCut &cut, const PromptParts &parts, unsigned block,
+__device__ __forceinline__ void join_dq(const PromptGeom &g, const PromptCut &cut, const PromptParts &parts, unsigned group,
                                         const float *__restrict__ mean, uint16_t *__restrict__ dQ)
 {
-    constexpr int N = D / 64;
-    const int lane = threadIdx.x & 63;
-    PartRow r;
-    if (!part_row(g, cut, parts, PB_BLOCK, (long long)block * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r)) return;
-    const float *from = parts.result + (size_t)r.kv * cut.cap * dq_part_floats(D);
-    float o[N], total = 0.f;
+    constexpr int N = D / 16 / 4;  // groups of four columns that a lane has
+    const int sub = threadIdx.x & 15;
+    const PartRow r = part_row(g, cut, parts, PB_BLOCK, group);
+    float total = 0.f;
+    f32x4 o[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) o[k] = 0.f;
-    for (int x = 0; x < r.n; x += 4) {  // four parts' loads at a time
-        float y[4][N], t[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const float *part = from + __builtin_amdgcn_readlane(r.item, min(x + u, r.n - 1)) * dq_part_floats(D);
-            t[u] = part[PB_BLOCK * D + r.at];
-#pragma unroll
-            for (int k = 0; k < N; ++k) y[u][k] = part[r.at * D + N * lane + k];
-        }
+    for (int k = 0; k < N; ++k) o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < r.most; x += 4) {
+        const float *at[4];
+        part_results(r, cut, parts, dq_part_floats(D), x, at);
+        float t[4];
+        f32x4 y[4][N];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            if (x + u >= r.n) break;
-            total += t[u];
+            t[u] = at[u][PB_BLOCK * D + r.at];
 #pragma unroll
-            for (int k = 0; k < N; ++k) o[k] += y[u][k];
+            for (int k = 0; k < N; ++k) y[u][k] = *reinterpret_cast<const f32x4 *>(at[u] + r.at * D + 4 * (N * sub + k));
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (x + u < r.n) {
+                total += t[u];
+#pragma unroll
+                for (int k = 0; k < N; ++k) o[k] += y[u][k];
+            }
     }
+    if (r.n == 0) return;
     const float c = 1.0f / sqrtf((float)D);
-    const float *m = mean + ((size_t)r.seq * g.Hkv + r.kv) * D + N * lane;
+    const float *m = mean + ((size_t)r.seq * g.Hkv + r.kv) * D + 4 * N * sub;
 #pragma unroll
-    for (int k = 0; k < N; ++k) reinterpret_cast<__bf16 *>(dQ)[(size_t)r.row * D + N * lane + k] = (__bf16)((o[k] - total * m[k]) * c);
+    for (int k = 0; k < N; ++k)
+        *reinterpret_cast<uint2 *>(dQ + r.row * D + 4 * (N * sub + k)) = pack_bf16((o[k] - total * *reinterpret_cast<const f32x4 *>(m + 4 * k)) * c);
 }
 
 // Key blocks of a sequence whose walk over the rows has at least t tiles of 64; the first blocks walk farthest.
@@ -744,7 +747,7 @@ static hipError_t launch_bwd(const PromptGeom &g, const uint16_t *Q, const uint1
                      : launch_products<D, true>(g, spans, key_grid, cut, w.rows, arg, st);
     if (e != hipSuccess) return e;
     const unsigned key_groups = g.Tk > 0 && spans.most > 1 ? (unsigned)(spans.blocks * g.Hkv * reduce_groups(D)) : 0u;
-    const unsigned row_groups = cut.cap > 0 ? (unsigned)((rows + 3) / 4) : 0u;
+    const unsigned row_groups = cut.cap > 0 ? join_groups(g) : 0u;
     if (key_groups + row_groups > 0)
         hipLaunchKernelGGL((prompt_bwd_join_kernel<D>), dim3(key_groups + row_groups), dim3(256), 0, st, g, spans, key_groups, cut, w.rows, arg);
     return hipGetLastError();
