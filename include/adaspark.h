@@ -377,8 +377,9 @@ int adaspark_ffn_sparse(const adaspark_shape *shape, const adaspark_ffn_dims *di
  *                   shared out to several workgroups; may then be NULL
  * Score products are exact in fp32 and the log-sum-exp is that of fp32 weights; the weights are rounded to bf16 (off by up to 2^-8 of each) for their
  * products with V.  K and V of a sequence have to be finite: a row may multiply the V of a key that it does not attend by a weight of 0.
- * Limits: head_dim in {64, 128}; q_heads/kv_heads <= 128; q_tokens*q_heads and k_tokens*kv_heads < 2^31, either number of tokens <= 2^30; strides multiples of 8 up to 2^22, and
- * at least heads*head_dim (otherwise ADASPARK_EINVAL).
+ * Outputs must not overlap inputs or each other (ADASPARK_EINVAL).
+ * Limits: head_dim in {64, 128}; q_heads/kv_heads <= 128; either number of tokens <= 2^30, and tokens*heads*head_dim/8 + 1024*sequences*kv_heads < 2^32 (the
+ * threads of a launch) for queries and for keys; strides multiples of 8 up to 2^22, and at least heads*head_dim (otherwise ADASPARK_EINVAL).
  */
 typedef struct {
     int32_t sequences;                    /* at least 1                                             */
@@ -423,7 +424,8 @@ int adaspark_prompt_attn_bwd(const adaspark_prompts *prompts, const void *Q, con
  * for a row of zeros); a code is the nearest value of the format to x / scale, and stands for code * scale.  A row that holds an
  * infinity or a NaN has a NaN for its scale.
  * Limits: page_size a power of two; table_pages*page_size <= 2^30; pages*page_size and page_size*kv_heads*head_dim < 2^31; q_heads, kv_heads, head_dim as above,
- * sequences*q_heads < 2^31 (the sequences of a decode step that share a KV head's keys with more than 16 query heads read them once per 16).
+ * sequences*q_heads <= 2^22, tokens*kv_heads*head_dim/8 of a write or read below 2^32 - 256.
+ * (More than 16 query heads to a KV head read its keys once per 16 in a decode step.)
  */
 typedef enum {
     ADASPARK_CACHE_BF16 = 0,
@@ -455,7 +457,7 @@ int adaspark_cache_write(const adaspark_cache *cache, int32_t tokens, const void
  * Reads histories back: K and V rows [start[s], start[s+1]) are the positions 0, 1, ... of sequence s, as bf16 (codes times scale,
  * rounded once; zero where there is no page).  The other rows of K and V are left as they were.  With start as k_start the result
  * feeds adaspark_prompt_attn for a follow-up turn.
- *   K, V       out  bf16 [tokens][kv_heads][head_dim], contiguous
+ *   K, V       out  bf16 [tokens][kv_heads][head_dim], contiguous; they must not overlap each other or the cache (ADASPARK_EINVAL)
  */
 int adaspark_cache_read(const adaspark_cache *cache, int32_t tokens, const int32_t *start, const int32_t *table,
                         const void *K_cache, const void *V_cache, const float *k_scale, const float *v_scale, void *K, void *V,
@@ -467,6 +469,7 @@ int adaspark_cache_read(const adaspark_cache *cache, int32_t tokens, const int32
  *   Q          in   bf16 [sequences][q_heads][head_dim];  O  out  likewise;  lse  out  fp32 [sequences][q_heads], or NULL
  *   workspace       adaspark_decode_workspace_bytes: partial results of sequences whose keys several workgroups share; 0 for
  *                   many sequences, may then be NULL
+ * O and lse must not overlap Q, the cache or each other (ADASPARK_EINVAL).
  * Positions that hold no token, and what lies in a page behind a sequence's length, may hold anything, NaN included.
  */
 int adaspark_decode_workspace_bytes(const adaspark_cache *cache, size_t *bytes);

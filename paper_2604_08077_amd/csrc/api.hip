@@ -82,12 +82,11 @@ int check_prompts(const adaspark_prompts *p)
     if (rc != ADASPARK_OK) return rc;
     for (const auto &x : {std::make_pair(p->q_stride, p->q_heads), std::make_pair(p->k_stride, p->kv_heads), std::make_pair(p->v_stride, p->kv_heads)})
         if ((rc = check_stride(x.first, x.second, p->head_dim)) != ADASPARK_OK) return rc;
-    if ((long long)p->q_tokens * p->q_heads >= (1ll << 31) || (long long)p->k_tokens * p->kv_heads >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
     if (p->q_heads / p->kv_heads > PROMPT_MAX_GROUP) return ADASPARK_EUNSUPPORTED;
     if (p->q_tokens > (1 << 30) || p->k_tokens > (1 << 30)) return ADASPARK_EUNSUPPORTED;
-    // the workgroups of a launch, with room for spans and parts
-    if (((long long)p->q_tokens * (p->q_heads / p->kv_heads) / 256 + p->sequences) * p->kv_heads >= (1ll << 24)) return ADASPARK_EUNSUPPORTED;
-    if (((long long)p->k_tokens / 256 + p->sequences) * p->kv_heads >= (1ll << 24)) return ADASPARK_EUNSUPPORTED;
+    // the threads of a launch: up to head_dim / 8 for a row, and several workgroups for a sequence and KV head
+    const long long own = 1024ll * p->sequences * p->kv_heads, most = (1ll << 32) - own, lanes = p->head_dim / 8;
+    if ((long long)p->q_tokens * p->q_heads * lanes >= most || (long long)p->k_tokens * p->kv_heads * lanes >= most) return ADASPARK_EUNSUPPORTED;
     return ADASPARK_OK;
 }
 
@@ -100,7 +99,7 @@ int check_cache(const adaspark_cache *c)
     if ((c->page_size & (c->page_size - 1)) != 0) return ADASPARK_EUNSUPPORTED;
     if ((long long)c->table_pages * c->page_size > (1ll << 30) || (long long)c->pages * c->page_size >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
     if ((long long)c->kv_heads * c->head_dim >= (1 << 24) || (long long)c->kv_heads * c->head_dim * c->page_size >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
-    if ((long long)c->sequences * c->q_heads >= (1ll << 31) || c->q_heads >= (1 << 16)) return ADASPARK_EUNSUPPORTED;
+    if ((long long)c->sequences * c->q_heads > (1ll << 22) || c->q_heads >= (1 << 16)) return ADASPARK_EUNSUPPORTED;
     return ADASPARK_OK;
 }
 
@@ -110,6 +109,12 @@ int check_cache_ptrs(const adaspark_cache *c, const void *K, const void *V, cons
     const int rc = check_ptrs({K, V});
     if (rc != ADASPARK_OK) return rc;
     return c->format == ADASPARK_CACHE_E4M3 ? check_ptrs({ks, vs}) : ks == nullptr && vs == nullptr ? ADASPARK_OK : ADASPARK_EINVAL;
+}
+
+// bytes of its keys, and of its values
+size_t cache_bytes(const adaspark_cache *c)
+{
+    return (size_t)c->pages * c->page_size * c->kv_heads * c->head_dim * (c->format == ADASPARK_CACHE_E4M3 ? 1 : 2);
 }
 
 bool aligned4(const void *p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -549,6 +554,15 @@ static int scratch_check(const void *workspace, size_t workspace_bytes, size_t n
     return workspace != nullptr && aligned16(workspace) && workspace_bytes >= need ? ADASPARK_OK : ADASPARK_EWORKSPACE;
 }
 
+// bytes from the first of a tensor's tokens to behind its last
+static size_t row_extent(int tokens, long long stride, int heads, int D) { return tokens > 0 ? ((size_t)(tokens - 1) * stride + (size_t)heads * D) * 2 : 0; }
+static bool overlaps_any(const void *p, size_t n, const std::pair<const void *, size_t> *others, int count)
+{
+    for (int i = 0; i < count; ++i)
+        if (n && others[i].second && overlap(p, n, others[i].first, others[i].second)) return true;
+    return false;
+}
+
 int adaspark_prompt_attn(const adaspark_prompts *prompts, const void *Q, const void *K, const void *V, const int32_t *q_start,
                          const int32_t *k_start, int causal, void *O, float *lse, void *workspace, size_t workspace_bytes,
                          void *stream)
@@ -557,10 +571,15 @@ int adaspark_prompt_attn(const adaspark_prompts *prompts, const void *Q, const v
     if (rc != ADASPARK_OK) return rc;
     if (!aligned4(q_start) || !aligned4(k_start)) return ADASPARK_EINVAL;
     const PromptGeom g = make_prompt_geom(*prompts, q_start, k_start, causal);
+    const int D = prompts->head_dim;
     if (g.Tq > 0 && (rc = check_ptrs({Q, O})) != ADASPARK_OK) return rc;
     if (g.Tk > 0 && (rc = check_ptrs({K, V})) != ADASPARK_OK) return rc;
     if (lse != nullptr && !aligned16(lse)) return ADASPARK_EINVAL;
-    if ((rc = scratch_check(workspace, workspace_bytes, prompt_workspace_bytes(g, prompts->head_dim))) != ADASPARK_OK) return rc;
+    if ((rc = scratch_check(workspace, workspace_bytes, prompt_workspace_bytes(g, D))) != ADASPARK_OK) return rc;
+    const size_t n = (size_t)g.Tq * g.Hq;
+    const std::pair<const void *, size_t> at[5] = {{Q, row_extent(g.Tq, g.qs, g.Hq, D)}, {K, row_extent(g.Tk, g.ks, g.Hkv, D)},
+                                                   {V, row_extent(g.Tk, g.vs, g.Hkv, D)}, {O, n * D * 2}, {lse, lse ? n * 4 : 0}};
+    if (overlaps_any(O, n * D * 2, at, 3) || overlaps_any(lse, at[4].second, at, 4)) return ADASPARK_EINVAL;
     if (g.Tq == 0) return ADASPARK_OK;
     const hipError_t e = launch_prompt_attn(g, prompts->head_dim, static_cast<const uint16_t *>(Q), static_cast<const uint16_t *>(K),
                                             static_cast<const uint16_t *>(V), static_cast<uint16_t *>(O), lse, workspace,
@@ -580,16 +599,12 @@ int adaspark_prompt_attn_bwd(const adaspark_prompts *prompts, const void *Q, con
     if (g.Tq > 0 && (rc = check_ptrs({Q, O, lse, dO, dQ})) != ADASPARK_OK) return rc;
     if (g.Tk > 0 && (rc = check_ptrs({K, V, dK, dV})) != ADASPARK_OK) return rc;
     if ((rc = scratch_check(workspace, workspace_bytes, prompt_bwd_workspace_bytes(g, D))) != ADASPARK_OK) return rc;
-    auto extent = [&](int tokens, long long stride, int heads) { return tokens > 0 ? ((size_t)(tokens - 1) * stride + (size_t)heads * D) * 2 : 0; };
     const size_t nq = (size_t)g.Tq * g.Hq * D * 2, nk = (size_t)g.Tk * g.Hkv * D * 2;
     const std::pair<const void *, size_t> outs[3] = {{dQ, nq}, {dK, nk}, {dV, nk}};
-    const std::pair<const void *, size_t> ins[6] = {{Q, extent(g.Tq, g.qs, g.Hq)}, {K, extent(g.Tk, g.ks, g.Hkv)}, {V, extent(g.Tk, g.vs, g.Hkv)},
-                                                    {O, nq}, {dO, nq}, {lse, (size_t)g.Tq * g.Hq * 4}};
+    const std::pair<const void *, size_t> ins[6] = {{Q, row_extent(g.Tq, g.qs, g.Hq, D)}, {K, row_extent(g.Tk, g.ks, g.Hkv, D)},
+                                                    {V, row_extent(g.Tk, g.vs, g.Hkv, D)}, {O, nq}, {dO, nq}, {lse, (size_t)g.Tq * g.Hq * 4}};
     for (int a = 0; a < 3; ++a) {
-        for (const auto &in : ins)
-            if (outs[a].second && in.second && overlap(outs[a].first, outs[a].second, in.first, in.second)) return ADASPARK_EINVAL;
-        for (int b = 0; b < a; ++b)
-            if (outs[a].second && outs[b].second && overlap(outs[a].first, outs[a].second, outs[b].first, outs[b].second)) return ADASPARK_EINVAL;
+        if (overlaps_any(outs[a].first, outs[a].second, ins, 6) || overlaps_any(outs[a].first, outs[a].second, outs, a)) return ADASPARK_EINVAL;
     }
     if (g.Tq == 0 && g.Tk == 0) return ADASPARK_OK;
     const hipError_t e = launch_prompt_bwd(g, D, static_cast<const uint16_t *>(Q), static_cast<const uint16_t *>(K),
@@ -610,7 +625,7 @@ int adaspark_cache_write(const adaspark_cache *cache, int32_t tokens, const void
     if (tokens > 0 && (rc = check_ptrs({K, V})) != ADASPARK_OK) return rc;
     if ((rc = check_stride(k_stride, cache->kv_heads, cache->head_dim)) != ADASPARK_OK) return rc;
     if ((rc = check_stride(v_stride, cache->kv_heads, cache->head_dim)) != ADASPARK_OK) return rc;
-    if ((long long)tokens * cache->kv_heads >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
+    if ((long long)tokens * cache->kv_heads * (cache->head_dim / 8) >= (1ll << 32) - CACHE_THREADS) return ADASPARK_EUNSUPPORTED;
     if (tokens == 0) return ADASPARK_OK;
     const long long contiguous = (long long)cache->kv_heads * cache->head_dim;
     const hipError_t e = launch_cache_write(make_cache_geom(*cache), tokens, static_cast<const uint16_t *>(K), k_stride ? k_stride : contiguous,
@@ -627,8 +642,11 @@ int adaspark_cache_read(const adaspark_cache *cache, int32_t tokens, const int32
     if (tokens < 0 || !aligned4(start) || !aligned4(table)) return ADASPARK_EINVAL;
     if ((rc = check_cache_ptrs(cache, K_cache, V_cache, k_scale, v_scale)) != ADASPARK_OK) return rc;
     if (tokens > 0 && (rc = check_ptrs({K, V})) != ADASPARK_OK) return rc;
-    if ((long long)tokens * cache->kv_heads >= (1ll << 31)) return ADASPARK_EUNSUPPORTED;
+    if ((long long)tokens * cache->kv_heads * (cache->head_dim / 8) >= (1ll << 32) - CACHE_THREADS) return ADASPARK_EUNSUPPORTED;
     if (tokens == 0) return ADASPARK_OK;
+    const size_t n = row_extent(tokens, (long long)cache->kv_heads * cache->head_dim, cache->kv_heads, cache->head_dim), held = cache_bytes(cache);
+    const std::pair<const void *, size_t> at[3] = {{K_cache, held}, {V_cache, held}, {K, n}};
+    if (overlaps_any(K, n, at, 2) || overlaps_any(V, n, at, 3)) return ADASPARK_EINVAL;
     const CacheData data{const_cast<void *>(K_cache), const_cast<void *>(V_cache), const_cast<float *>(k_scale), const_cast<float *>(v_scale)};
     const hipError_t e = launch_cache_read(make_cache_geom(*cache), tokens, start, table, data, static_cast<uint16_t *>(K),
                                            static_cast<uint16_t *>(V), static_cast<hipStream_t>(stream));
@@ -656,6 +674,9 @@ int adaspark_decode_attn(const adaspark_cache *cache, const void *Q, const int32
     if ((rc = check_cache_ptrs(cache, K_cache, V_cache, k_scale, v_scale)) != ADASPARK_OK) return rc;
     const CacheGeom g = make_cache_geom(*cache);
     if ((rc = scratch_check(workspace, workspace_bytes, decode_workspace_bytes(g))) != ADASPARK_OK) return rc;
+    const size_t n = (size_t)g.B * g.Hq * g.D * 2, held = cache_bytes(cache);
+    const std::pair<const void *, size_t> at[4] = {{Q, n}, {K_cache, held}, {V_cache, held}, {O, n}};
+    if (overlaps_any(O, n, at, 3) || overlaps_any(lse, lse ? (size_t)g.B * g.Hq * 4 : 0, at, 4)) return ADASPARK_EINVAL;
     const CacheData data{const_cast<void *>(K_cache), const_cast<void *>(V_cache), const_cast<float *>(k_scale), const_cast<float *>(v_scale)};
     const hipError_t e = launch_decode_attn(g, static_cast<const uint16_t *>(Q), table, lengths, data, static_cast<uint16_t *>(O), lse, workspace,
                                             static_cast<hipStream_t>(stream));

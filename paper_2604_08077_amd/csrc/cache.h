@@ -9,6 +9,8 @@
 
 namespace adaspark {
 
+constexpr int CACHE_THREADS = 256;  // of a workgroup of the write and read kernels
+
 struct CacheGeom {
     int B, pages, shift, table_pages;  // page_size = 1 << shift
     int Hq, Hkv, G, D;

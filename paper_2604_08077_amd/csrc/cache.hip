@@ -9,7 +9,6 @@ namespace adaspark {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int CACHE_THREADS = 256;
 constexpr int STARTS_LDS = 1024;  // starts held in LDS; with more sequences they are searched in memory
 
 // The sequence of token t: the last s with starts[s] <= t, -1 if t lies in none.  Whatever starts holds, the result is in

@@ -309,7 +309,8 @@ __device__ __forceinline__ PartRow part_row(const PromptGeom &g, const PromptCut
     r.item += id * PARTS_MAX;
     const int n = min(parts.count[id], PARTS_MAX);
     r.n = a < g.Hq && n > 1 ? n : 0;
-    r.most = max(max(__builtin_amdgcn_readlane(r.n, 0), __builtin_amdgcn_readlane(r.n, 16)), max(__builtin_amdgcn_readlane(r.n, 32), __builtin_amdgcn_readlane(r.n, 48)));
+    r.most = max(max(__builtin_amdgcn_readlane(r.n, 0), __builtin_amdgcn_readlane(r.n, 16)),
+                 max(__builtin_amdgcn_readlane(r.n, 32), __builtin_amdgcn_readlane(r.n, 48)));
     return r;
 }
 // Where the results of parts x .. x + 3 of the lane's row lie, of `floats` each (past its last part the last one's again; starts that overlap

@@ -10,8 +10,9 @@
 // Bound by the matrix pipes and, at head-dim 64, by the exponentials and what surrounds them (an exponential, a multiply-add, an addition
 // and half a conversion for each score).  Two workgroups on a CU (three at head-dim 64) are not in step, so one's softmax, barriers and
 // first loads run under the other's products.  A workgroup of eight wavefronts with 256 rows and three stages, its two halves in counter-phase as in
-// attn_walk.hip, is as fast at head-dim 128 on long walks (32,768 tokens of 28/4 heads 6.0 ms either way) and slower on short ones (16 prompts of
-// 17 to 1,504 tokens 87 us, so 82) and at head-dim 64 (32,768 tokens of 8/2 heads 1.32 ms, 1.07; 4,096 85 us, 59).
+// attn_walk.hip, is as fast at head-dim 128 on long walks (32,768 tokens of 28/4 heads 5.8 ms either way, 1.26 PF/s, where the clock is held down by
+// power) and slower on short ones (16 prompts of 17 to 1,504 tokens 1.06 times as long) and at head-dim 64 (32,768 tokens of 8/2 heads 1.32 ms, 1.07;
+// 4,096 85 us, 59).
 //
 // Score products are exact (bf16 x bf16 accumulated in fp32); the softmax scale is applied in fp32 with the reference, one
 // instruction.  Weights are rounded to bf16 for P.V only: the sum is of the fp32 weights, so the log-sum-exp carries no bf16 rounding.

@@ -20,8 +20,8 @@
 // Where few key blocks have long walks, a walk is cut into spans, a workgroup each, which leave fp32 sums in the
 // workspace; prompt_bwd_join_kernel adds them in their order.  Walks of few row blocks are shared out as in the forward (prompt.h).
 //
-// Workgroups of four wavefronts and two stages, two to a CU, which are not in step (a training pass over 16k tokens in 5 sequences of 28/4 heads
-// of 128, in ms, with eight wavefronts and three stages 2.31, so 2.20).
+// Workgroups of four wavefronts and two stages, two to a CU, which are not in step; eight wavefronts and three stages take 1.05 times as long (a
+// training pass over 16k tokens in 5 sequences of 28/4 heads of 128: 2.01 ms, 870 TF/s).
 #include <algorithm>
 
 #include "prompt.h"
@@ -39,9 +39,8 @@ struct PromptBwd {
     static constexpr int PER = 64 / RPI / PB_WAVES;  // direct-to-LDS instructions per wavefront, tile and operand
     static constexpr int OFF_LSE = 2 * TILE;  // behind the two tiles (dK/dV kernel): 64 start values of S, 64 of dP
     static constexpr int STAGE = 2 * TILE + 512;
-    static constexpr int NST = PB_WAVES == 8 ? 3 : 2;
-    static constexpr int BYTES = NST * STAGE;
-    static_assert(BYTES <= 160 * 1024, "LDS of one CU");
+    static constexpr int BYTES = 2 * STAGE;
+    static_assert(BYTES <= 80 * 1024, "half the LDS of a CU");
 };
 
 // ---- the spans of the dK/dV kernel: row tiles of a workgroup.  How long they are follows from the lengths, which the device knows
@@ -73,7 +72,7 @@ __device__ __forceinline__ int span_tiles(const PromptGeom &g, int most)
     for (int s = threadIdx.x & 63; s < g.B; s += 64) {
         const PromptSeq p = prompt_seq(g, s);
         const long long rows = (long long)p.n * g.G, nb = (p.m + PB_BLOCK - 1) / PB_BLOCK, off = p.m - p.n;
-        // block j's walk begins at row G * max(0, 256 j - off)
+        // block j's walk begins at row G * max(0, 128 j - off)
         const long long z = g.causal ? min(nb, max(0ll, off / PB_BLOCK + (off >= 0 ? 1 : 0))) : nb, rest = nb - z;
         total += (float)nb * (float)rows - (float)g.G * ((float)(PB_BLOCK * (z + nb - 1)) * 0.5f - (float)off) * (float)rest;
         if (p.m > 0) longest = max(longest, (int)((rows - (g.causal ? min(rows, max(0ll, -off) * g.G) : 0) + 63) / 64));
@@ -94,7 +93,7 @@ struct PromptBwdWorkspace {
     float *mean;          // [B][Hkv][D] of 64 keys of each sequence
     PromptParts rows;     // parts of the dQ kernel's walks
     float *lse2, *delta;  // [Tq * Hq + 1]: entry [Tq * Hq] belongs to the rows that pad a tile: -inf, 0
-    float *part;          // [Hkv][blocks][most][2 (dV, dK)][256 x D] in MFMA output order
+    float *part;          // [Hkv][blocks][most][2 (dV, dK)][128 x D] in MFMA output order
     size_t bytes;
 };
 static PromptBwdWorkspace bwd_workspace_of(const PromptGeom &g, int D, void *ws)

@@ -133,3 +133,38 @@ def test_tensors_that_are_refused():
         B.decode_attn(csh, Q[:1], c, table, lengths)
     with pytest.raises(B.AdasparkError):
         B.decode_workspace_bytes(B.CacheShape(1, 2, 16, 2, 4, 2, 64, "int4"))
+
+
+def test_outputs_that_overlap_are_refused(lib):
+    c, size = prompts(), 8 * 4 * 64 * 2
+    Q, K, V, O, lse = (P + i * 2 * size for i in range(5))
+    call = lambda o, l=None: lib.adaspark_prompt_attn(ctypes.byref(c), Q, K, V, P, P, 1, o, l, None, 0, None)  # noqa: E731
+    for o, l in ((Q, None), (K + 16, None), (V - size + 16, None), (O, Q), (O, V + 64), (O, O + size - 16)):
+        assert call(o, l) == EINVAL, (o, l)
+    few = prompts(q_tokens=0, k_tokens=0)  # (no element, no overlap)
+    assert lib.adaspark_prompt_attn(ctypes.byref(few), Q, K, V, P, P, 1, Q, None, None, 0, None) == OK
+    for fmt, scale in ((0, None), (1, P)):
+        c = cache(format=fmt)
+        held, rows = c.pages * c.page_size * c.kv_heads * c.head_dim * (2 - fmt), 4 * c.kv_heads * c.head_dim * 2
+        Kc, Vc, K, V = P << 4, P << 5, P << 6, P << 7
+        for k, v in ((Kc + held - 16, V), (K, Vc), (K, K + rows - 16), (K, K), (Vc - rows + 16, V)):
+            assert lib.adaspark_cache_read(ctypes.byref(c), 4, P, P, Kc, Vc, scale, scale, k, v, None) == EINVAL
+        q = c.sequences * c.q_heads * c.head_dim * 2
+        for o, l in ((K, None), (K + q - 16, None), (Kc + held - 16, None), (Vc, None), (V, K), (V, V + 16), (V, Kc)):
+            assert lib.adaspark_decode_attn(ctypes.byref(c), K, P, P, Kc, Vc, scale, scale, o, l, P << 8, 1 << 40, None) == EINVAL
+
+
+def test_more_threads_than_a_launch_has(lib):
+    n = ctypes.c_size_t(0)
+    size = lambda **kw: lib.adaspark_prompt_workspace_bytes(ctypes.byref(prompts(**kw)), 1, 1, ctypes.byref(n))  # noqa: E731
+    one = dict(sequences=1, q_heads=1, kv_heads=1, head_dim=128)
+    assert size(**one, q_tokens=1 << 28, k_tokens=8) == EUNSUPPORTED
+    assert size(**one, q_tokens=(1 << 28) - 65, k_tokens=(1 << 28) - 65) == OK
+    assert size(**one, q_tokens=8, k_tokens=1 << 28) == EUNSUPPORTED
+    assert size(sequences=1 << 20, q_heads=4, kv_heads=4, head_dim=64, q_tokens=8, k_tokens=8) == EUNSUPPORTED
+    assert size(sequences=1 << 20, q_heads=2, kv_heads=2, head_dim=64, q_tokens=1 << 20, k_tokens=1 << 20) == OK
+    decode = lambda **kw: lib.adaspark_decode_workspace_bytes(ctypes.byref(cache(**kw)), ctypes.byref(n))  # noqa: E731
+    assert decode(sequences=1 << 20, q_heads=4, kv_heads=4) == OK and decode(sequences=(1 << 20) + 1, q_heads=4, kv_heads=4) == EUNSUPPORTED
+    c = cache(q_heads=1, kv_heads=1, head_dim=128)
+    assert lib.adaspark_cache_write(ctypes.byref(c), 1 << 28, P, 0, P, 0, P, P, P, P, P, None, None, None) == EUNSUPPORTED
+    assert lib.adaspark_cache_read(ctypes.byref(c), 1 << 28, P, P, P, P, None, None, P, P, None) == EUNSUPPORTED
