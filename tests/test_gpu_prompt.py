@@ -260,3 +260,45 @@ def test_other_stream_and_replayed_graphs(B):
             graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((O, lse, *grads), eager[which]))
+
+
+@pytest.mark.parametrize("heads", [(7, 1, 64), (128, 1, 64), (6, 6, 128), (28, 4, 128)])
+@pytest.mark.parametrize("q_len,k_len,causal", [([1], [40001], True), ([3, 0, 2], [5000, 70, 9001], True), ([9, 1], [6400, 20000], False)])
+def test_few_rows_on_many_keys(B, heads, q_len, k_len, causal):
+    """Walks shared out to up to 64 workgroups; groups of heads that are no multiple of what a wavefront joins at once."""
+    tq, tk = sum(q_len), sum(k_len)
+    Q, K, V, dO = inputs(heads, tq, tk, 31)
+    sh = B.PromptShape(len(q_len), tq, tk, *heads)
+    assert B.prompt_workspace_bytes(sh, B.PROMPT_ATTN, causal) > 0
+    qs, ks = R.starts(q_len).cuda(), R.starts(k_len).cuda()
+    O, lse = B.prompt_attn(sh, Q, K, V, qs, ks, causal=causal, return_lse=True)
+    check_forward(O, lse, R.attention(Q, K, V, q_len, k_len, causal), max(k_len))
+    got = B.prompt_attn_bwd(sh, Q, K, V, O, lse, dO, qs, ks, causal=causal)
+    want, tol = R.gradients(Q, K, V, O, lse, dO, q_len, k_len, causal)
+    for name, x in zip(("dQ", "dK", "dV"), got):
+        worst = float(((x.double() - want[name]).abs() / tol[name]).max())
+        assert worst <= 1, f"{name}: {worst:.2f} of its bound"
+
+
+def test_calls_at_once(B):
+    """Two streams with a workspace each: what either gives is what it gives alone."""
+    jobs = []
+    for i, (heads, q_len, k_len) in enumerate([((8, 2, 64), [50, 7], [6000, 300]), ((6, 2, 128), [700, 333], [700, 333])]):
+        data = inputs(heads, sum(q_len), sum(k_len), 50 + i)
+        jobs.append((B.PromptShape(2, sum(q_len), sum(k_len), *heads), data, R.starts(q_len).cuda(), R.starts(k_len).cuda(), torch.cuda.Stream()))
+
+    def both(sh, data, qs, ks):
+        O, lse = B.prompt_attn(sh, *data[:3], qs, ks, return_lse=True)
+        return (O, lse, *B.prompt_attn_bwd(sh, *data[:3], O, lse, data[3], qs, ks))
+
+    alone = [both(*job[:4]) for job in jobs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = [None, None]
+        for i, job in enumerate(jobs):
+            with torch.cuda.stream(job[4]):
+                for _ in range(3):
+                    got[i] = both(*job[:4])
+        torch.cuda.synchronize()
+        for x, y in zip(alone, got):
+            assert all(torch.equal(a, b) for a, b in zip(x, y))
