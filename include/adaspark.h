@@ -378,7 +378,7 @@ int adaspark_ffn_sparse(const adaspark_shape *shape, const adaspark_ffn_dims *di
  * Score products are exact in fp32 and the log-sum-exp is that of fp32 weights; the weights are rounded to bf16 (off by up to 2^-8 of each) for their
  * products with V.  K and V of a sequence have to be finite: a row may multiply the V of a key that it does not attend by a weight of 0.
  * Outputs must not overlap inputs or each other (ADASPARK_EINVAL).
- * Limits: head_dim in {64, 128}; q_heads/kv_heads <= 128; either number of tokens <= 2^30, and tokens*heads*head_dim/8 + 1024*sequences*kv_heads < 2^32 (the
+ * Limits: head_dim in {64, 128}; q_heads/kv_heads <= 128; either number of tokens <= 2^30, and tokens*heads*head_dim/8 + 1280*sequences*q_heads < 2^32 (the
  * threads of a launch) for queries and for keys; strides multiples of 8 up to 2^22, and at least heads*head_dim (otherwise ADASPARK_EINVAL).
  */
 typedef struct {
@@ -400,7 +400,7 @@ int adaspark_prompt_attn(const adaspark_prompts *prompts, const void *Q, const v
                          void *stream);
 
 /*
- * Its backward pass, with delta = dO.O per row:
+ * Its backward pass, with delta = dO.O per row, and in rows of up to 64 keys delta = sum_j p_j dO.v_j, the same but for the rounding of O:
  *   dV_j = sum p_j dO,  dS_j = p_j (dO.v_j - delta),  dQ = sum_j dS_j k_j / sqrt(head_dim),  dK_j = sum dS_j q / sqrt(head_dim)
  * (dK, dV summed over all rows and all query heads of the KV head's group).  sum_j dS_j is 0 in a row but for what the rounding of
  * O leaves in delta; dQ is taken as sum_j dS_j (k_j - r) / sqrt(head_dim) with r the mean of up to 64 keys of the sequence, which keeps that

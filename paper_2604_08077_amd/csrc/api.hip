@@ -84,8 +84,8 @@ int check_prompts(const adaspark_prompts *p)
         if ((rc = check_stride(x.first, x.second, p->head_dim)) != ADASPARK_OK) return rc;
     if (p->q_heads / p->kv_heads > PROMPT_MAX_GROUP) return ADASPARK_EUNSUPPORTED;
     if (p->q_tokens > (1 << 30) || p->k_tokens > (1 << 30)) return ADASPARK_EUNSUPPORTED;
-    // the threads of a launch: up to head_dim / 8 for a row, and several workgroups for a sequence and KV head
-    const long long own = 1024ll * p->sequences * p->kv_heads, most = (1ll << 32) - own, lanes = p->head_dim / 8;
+    // the threads of a launch: up to head_dim / 8 for a row, and several workgroups for a sequence and head
+    const long long own = 1280ll * p->sequences * p->q_heads, most = (1ll << 32) - own, lanes = p->head_dim / 8;
     if ((long long)p->q_tokens * p->q_heads * lanes >= most || (long long)p->k_tokens * p->kv_heads * lanes >= most) return ADASPARK_EUNSUPPORTED;
     return ADASPARK_OK;
 }

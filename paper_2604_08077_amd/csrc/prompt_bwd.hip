@@ -17,6 +17,10 @@
 // dQ (two MFMAs a tile against 96) and that many r taken off at the end, r the mean of 64 keys of the sequence: the error of dQ
 // against 64 bits, keys of as much common as own direction, goes from 4.0e-3 to 2.6e-3.
 //
+// Rows of up to FEW_KEYS keys, where gradients are largest and the rounding of O weighs most: delta = sum_j p_j (dO.v_j) in fp32, which is
+// dO.O without that rounding (one tile; early_delta).  Errors of dQ and dK against 64 bits in short sequences 2.7e-3 either, so 2.4e-3; rounding the outputs
+// alone leaves 1.7e-3.  1 to 2 us of a pass.
+//
 // Where few key blocks have long walks, a walk is cut into spans, a workgroup each, which leave fp32 sums in the
 // workspace; prompt_bwd_join_kernel adds them in their order.  Walks of few row blocks are shared out as in the forward (prompt.h).
 //
@@ -118,14 +122,71 @@ static PromptBwdWorkspace bwd_workspace_of(const PromptGeom &g, int D, void *ws)
 }
 size_t prompt_bwd_workspace_bytes(const PromptGeom &g, int D) { return bwd_workspace_of(g, D, nullptr).bytes; }
 
-// Start values of every row: 256 / (D / 8) rows to a workgroup, D / 8 lanes to a row.  A row without keys (log-sum-exp -inf) gets
-// no part in anything.  The first B * Hkv workgroups leave the mean keys, a thread to a column of some of the keys;
-// the very first wavefront also the length of a span.
+constexpr int FEW_KEYS = 64;
+// The tokens of a sequence with 1 .. FEW_KEYS keys.
+__device__ __forceinline__ void few_keys_of(const PromptGeom &g, int n, int m, int &from, int &to)
+{
+    from = g.causal ? max(0, n - m) : 0;
+    to = g.causal ? min((long long)n, (long long)n - m + FEW_KEYS) : m <= FEW_KEYS ? n : 0;
+    if (m == 0) to = from;
+}
+
+// -delta of such rows, of one sequence and KV head: 16 rows at a time, every `per`-th 16 from the c-th on.  S^T = K.Q^T and dP^T = V.dO^T, 16 keys
+// to a wavefront, operands straight from memory (a lane's: 16 bytes of a row), all asked for at once.
+constexpr int EARLY_ROWS = 16;
+inline int early_groups(const PromptGeom &g)  // workgroups for a sequence and KV head: what one twice as long as the average has
+{
+    const long long all = (long long)FEW_KEYS * g.G / EARLY_ROWS, even = (2ll * g.Tq * g.G / g.B + EARLY_ROWS - 1) / EARLY_ROWS;
+    return (int)std::max(1ll, std::min(all, even));
+}
 template <int D>
-__global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most, int *__restrict__ span, const uint16_t *__restrict__ K,
-                                                          float *__restrict__ mean, long long rows, const uint16_t *__restrict__ O, const uint16_t *__restrict__ dO,
-                                                          const float *__restrict__ lse, float *__restrict__ lse2,
-                                                          float *__restrict__ delta)
+__device__ __forceinline__ void early_delta(const PromptGeom &g, int s, int kv, int c, int per, const uint16_t *__restrict__ Q, const uint16_t *__restrict__ K,
+                                            const uint16_t *__restrict__ V, const uint16_t *__restrict__ dO, const float *__restrict__ lse,
+                                            float *__restrict__ delta)
+{
+    constexpr int KSTEPS = D / 32;
+    static_assert(FEW_KEYS == 4 * 16, "four wavefronts");
+    __shared__ float sums[4][EARLY_ROWS];
+    const int lane = threadIdx.x & 63, n16 = lane & 15, q4 = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const PromptSeq p = prompt_seq(g, s);
+    int from, to;
+    few_keys_of(g, p.n, p.m, from, to);
+    const float c2 = 1.44269504088896340736f / sqrtf((float)D);
+    for (int row0 = from * g.G + EARLY_ROWS * c; row0 < to * g.G; row0 += EARLY_ROWS * per) {
+        const int row = row0 + n16, r = min(row, to * g.G - 1), tok = token_of_row(g, r), head = kv * g.G + (r - tok * g.G);
+        const size_t id = (size_t)(p.q0 + tok) * g.Hq + head, key = (size_t)(p.k0 + min(16 * wave + n16, p.m - 1));
+        const int keys = g.causal ? p.m - p.n + tok + 1 : p.m;  // of the row: at least one
+        f32x4 sa = {0.f, 0.f, 0.f, 0.f}, pa = sa;
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k) {
+            const int d = 8 * q4 + 32 * k;
+            sa = mfma16(*reinterpret_cast<const bf16x8 *>(K + key * g.ks + (size_t)kv * D + d),
+                        *reinterpret_cast<const bf16x8 *>(Q + (size_t)(p.q0 + tok) * g.qs + (size_t)head * D + d), sa);
+            pa = mfma16(*reinterpret_cast<const bf16x8 *>(V + key * g.vs + (size_t)kv * D + d), *reinterpret_cast<const bf16x8 *>(dO + id * D + d), pa);
+        }
+        const float l2 = lse[id] * 1.44269504088896340736f;
+        float sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            if (16 * wave + 4 * q4 + v < keys) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(sa[v], c2, -l2)), pa[v], sum);
+        sum = quad_sum(sum);
+        if (q4 == 0) sums[wave][n16] = sum;
+        __syncthreads();
+        if (threadIdx.x < EARLY_ROWS && row < to * g.G)
+            delta[id] = l2 == -INFINITY ? 0.f : -((sums[0][n16] + sums[1][n16]) + (sums[2][n16] + sums[3][n16]));
+        __syncthreads();
+    }
+}
+
+// Start values of every row: 256 / (D / 8) rows to a workgroup, D / 8 lanes to a row.  A row without keys (log-sum-exp -inf) gets
+// no part in anything.  The first B * Hkv workgroups leave the mean keys, a thread to a column of some of the keys, the
+// very first wavefront also the length of a span; the next B * Hkv * early on the rows with few keys.
+template <int D>
+__global__ __launch_bounds__(256, 4) void prompt_prep_kernel(PromptGeom g, int most, int early, int *__restrict__ span, const uint16_t *__restrict__ Q,
+                                                          const uint16_t *__restrict__ K, const uint16_t *__restrict__ V,
+                                                          float *__restrict__ mean, long long rows, const uint16_t *__restrict__ O,
+                                                          const uint16_t *__restrict__ dO, const float *__restrict__ lse,
+                                                          float *__restrict__ lse2, float *__restrict__ delta)
 {
     constexpr int CPR = D / 8;
     if (blockIdx.x == 0 && threadIdx.x < 64) {
@@ -159,8 +220,15 @@ __global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most
         }
         return;
     }
-    const long long r = ((long long)(blockIdx.x - means) * 256 + threadIdx.x) / CPR;
-    const int col = threadIdx.x % CPR;
+    const unsigned skip = means * (unsigned)(1 + early);
+    if (blockIdx.x < skip) {
+        const unsigned x = (blockIdx.x - means) / (unsigned)early;
+        early_delta<D>(g, (int)(x / (unsigned)g.Hkv), (int)(x % (unsigned)g.Hkv), (int)((blockIdx.x - means) % (unsigned)early), early, Q, K, V, dO,
+                       lse, delta);
+        return;
+    }
+    const long long r = ((long long)(blockIdx.x - skip) * 256 + threadIdx.x) / CPR;
+    const int col = threadIdx.x % CPR, lane = threadIdx.x & 63;
     float part = 0.f;
     if (r < rows) {
         const bf16x8 a = *reinterpret_cast<const bf16x8 *>(dO + r * D + col * 8), b = *reinterpret_cast<const bf16x8 *>(O + r * D + col * 8);
@@ -169,11 +237,26 @@ __global__ __launch_bounds__(256) void prompt_prep_kernel(PromptGeom g, int most
     }
 #pragma unroll
     for (int d = CPR / 2; d >= 1; d >>= 1) part += __shfl_xor(part, d, 64);
-    if (col == 0 && r <= rows) {
-        const float l = r < rows ? lse[r] : -INFINITY;
-        lse2[r] = l == -INFINITY ? -INFINITY : -l * sqrtf((float)D);  // = -(lse in base 2) / (softmax scale in base 2)
-        delta[r] = -part;
+    // the row's sequence: the last one with a start at or before its token
+    const int tok = (int)((unsigned)min(r, rows) / (unsigned)g.Hq);
+    int seq = 0;
+    for (int s = 0; s < g.B; s += 64) {
+        const int start = g.q_start[min(s + lane, g.B - 1)];
+        unsigned long long last = 0ull;
+#pragma unroll
+        for (int j = 0; j < 64 / CPR; ++j) {
+            last = __ballot(s + lane < g.B && start <= __builtin_amdgcn_readlane(tok, j * CPR));
+            if (lane / CPR == j && last != 0ull) seq = s + 63 - __clzll(last);
+        }
+        if (last != ~0ull) break;  // (the wavefront's last row has the last of their sequences)
     }
+    if (col != 0 || r > rows) return;
+    const float l = r < rows ? lse[r] : -INFINITY;
+    lse2[r] = l == -INFINITY ? -INFINITY : -l * sqrtf((float)D);  // = -(lse in base 2) / (softmax scale in base 2)
+    const PromptSeq p = prompt_seq(g, seq);
+    int from, to;
+    few_keys_of(g, p.n, p.m, from, to);
+    if (r == rows || tok - p.q0 < from || tok - p.q0 >= to) delta[r] = -part;
 }
 
 struct PromptBwdArgs {
@@ -736,8 +819,9 @@ static hipError_t launch_bwd(const PromptGeom &g, const uint16_t *Q, const uint1
     const PromptCut cut = prompt_cut(g, PB_BLOCK, D);
     const PromptBwdArgs arg{Q, K, V, dO, w.lse2, w.delta, w.mean, w.span, w.part, dQ, dK, dV};
     const long long rows = (long long)g.Tq * g.Hq, per = 256 / (D / 8);
-    hipLaunchKernelGGL((prompt_prep_kernel<D>), dim3((unsigned)((long long)g.B * g.Hkv + (rows + 1 + per - 1) / per)), dim3(256), 0, st, g,
-                       spans.most, w.span, K, w.mean, rows, O, dO, lse, w.lse2, w.delta);
+    const int early = early_groups(g);
+    hipLaunchKernelGGL((prompt_prep_kernel<D>), dim3((unsigned)((long long)g.B * g.Hkv * (1 + early) + (rows + 1 + per - 1) / per)), dim3(256), 0, st, g,
+                       spans.most, early, w.span, Q, K, V, w.mean, rows, O, dO, lse, w.lse2, w.delta);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     // (a multiple of 8: the row blocks' workgroups keep their XCDs)

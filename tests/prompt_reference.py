@@ -55,7 +55,8 @@ def gradients(Q, K, V, O, lse, dO, q_len, k_len, causal=True):
     """The formulas of the backward on the O and lse that it is given -> fp64 dQ, dK, dV and their bounds.
 
     sum_j dS_j = sum_j p_j dP_j - delta is 0 for the delta that belongs to p; with delta from an O rounded to bf16 something is left of it, and the
-    library takes that out of dQ along r, the mean of up to 64 keys of the sequence: dQ = c sum_j dS_j (k_j - r)."""
+    library takes that out of dQ along r, the mean of up to 64 keys of the sequence: dQ = c sum_j dS_j (k_j - r).  In rows of up to 64 keys
+    delta is that sum."""
     Hq, D, Hkv = Q.shape[1], Q.shape[2], K.shape[1]
     G, c = Hq // Hkv, 1 / math.sqrt(Q.shape[2])
     out = {n: torch.zeros(t.shape, dtype=torch.float64, device=Q.device) for n, t in (("dQ", Q), ("dK", K), ("dV", V))}
@@ -73,9 +74,15 @@ def gradients(Q, K, V, O, lse, dO, q_len, k_len, causal=True):
                 s = s.masked_fill(torch.arange(m, device=s.device) > (m - n + torch.arange(n, device=s.device))[:, None], -math.inf)
             p = torch.where(torch.isneginf(l)[:, None], torch.zeros_like(s), torch.exp(s - l[:, None]))
             dp, delta = g @ v.T, (g * o).sum(-1, keepdim=True)
-            ds = p * (dp - delta)
             off = U32 * ((D + 4) * big + 4 * l.abs().nan_to_num(posinf=0.0)[:, None] + 16)      # of p, relative
             ddp = U32 * (D + 4) * (g.abs() @ v.abs().T + (g * o).abs().sum(-1, keepdim=True))   # of dp - delta
+            # rows of up to 64 keys: off by p's and dP's errors, and those of up to 64 products and sums
+            few_keys = (torch.ones_like(p).masked_fill(torch.isneginf(s), 0).sum(-1, keepdim=True) <= 64)
+            delta = torch.where(few_keys, (p * dp).sum(-1, keepdim=True), delta)
+            e_dp = U32 * (D + 4) * (g.abs() @ v.abs().T)
+            e_delta = (p * (e_dp + dp.abs() * off)).sum(-1, keepdim=True) + U32 * 72 * (p * dp.abs()).sum(-1, keepdim=True)
+            ddp = torch.where(few_keys, e_dp + e_delta + U32 * (dp.abs() + delta.abs()), ddp)
+            ds = p * (dp - delta)
             e_ds = ds.abs() * (U16 + off) + p * ddp * (1 + U16)                                 # dS in bf16
             e_p = p * (U16 + off)
             few = min(m, 64)
