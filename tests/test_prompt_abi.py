@@ -159,7 +159,7 @@ def test_more_threads_than_a_launch_has(lib):
     size = lambda **kw: lib.adaspark_prompt_workspace_bytes(ctypes.byref(prompts(**kw)), 1, 1, ctypes.byref(n))  # noqa: E731
     one = dict(sequences=1, q_heads=1, kv_heads=1, head_dim=128)
     assert size(**one, q_tokens=1 << 28, k_tokens=8) == EUNSUPPORTED
-    assert size(**one, q_tokens=(1 << 28) - 65, k_tokens=(1 << 28) - 65) == OK
+    assert size(**one, q_tokens=(1 << 28) - 81, k_tokens=(1 << 28) - 81) == OK
     assert size(**one, q_tokens=8, k_tokens=1 << 28) == EUNSUPPORTED
     assert size(sequences=1 << 20, q_heads=4, kv_heads=4, head_dim=64, q_tokens=8, k_tokens=8) == EUNSUPPORTED
     assert size(sequences=1 << 20, q_heads=2, kv_heads=2, head_dim=64, q_tokens=1 << 20, k_tokens=1 << 20) == OK
