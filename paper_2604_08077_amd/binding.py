@@ -72,8 +72,7 @@ class _CPrompts(ctypes.Structure):
         (n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")]
 
 
-@dataclass(frozen=True)
-class PromptShape:
+class PromptShape(NamedTuple):
     """Packed prompts: mirror of ``adaspark_prompts`` but for the strides, which the calls take from the tensors."""
 
     sequences: int
@@ -96,8 +95,7 @@ class _CCache(ctypes.Structure):
 CACHE_FORMATS = {"bf16": 0, "e4m3": 1}  # adaspark_cache_format
 
 
-@dataclass(frozen=True)
-class CacheShape:
+class CacheShape(NamedTuple):
     """Mirror of ``adaspark_cache``; ``format``: "bf16" or "e4m3"."""
 
     sequences: int
@@ -559,7 +557,7 @@ def cube_select_shared(shape: Shape, Q: torch.Tensor, kbar: torch.Tensor, top_p:
 
 
 def _device(t: torch.Tensor, name: str) -> int:
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor (this package has no CPU path)")
     return t.get_device()
 
@@ -584,6 +582,11 @@ def _rows_at(t, dev: int, tokens: int, heads: int, head_dim: int, name: str) -> 
     if one != 1 or (heads > 1 and head != head_dim) or (tokens > 1 and step < heads * head_dim):
         raise ValueError(f"{name}: the heads of a token have to lie one behind the other, got strides {t.stride()}")
     return t.data_ptr(), step if tokens > 1 else 0
+
+
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor of the size and type of a (checked) bf16 [tokens, heads, head_dim]; the shortest call for it."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _run(dev: int, fn_name: str, *args) -> None:
@@ -637,7 +640,7 @@ def prompt_attn(shape: PromptShape, Q, K, V, q_start, k_start=None, causal: bool
     dev = _device(Q, "Q")
     q, k, v = _rows_at(Q, dev, Tq, Hq, D, "Q"), _rows_at(K, dev, Tk, Hkv, D, "K"), _rows_at(V, dev, Tk, Hkv, D, "V")
     if O is None:
-        O = torch.empty((Tq, Hq, D), dtype=torch.bfloat16, device=Q.device)
+        O = _like(Q)
     if lse is None and return_lse:
         lse = torch.empty((Tq, Hq), dtype=torch.float32, device=Q.device)
     ws, ws_ptr, ws_bytes = _scratch(prompt_workspace_bytes(shape, PROMPT_ATTN, causal), workspace, Q, dev)
@@ -655,9 +658,9 @@ def prompt_attn_bwd(shape: PromptShape, Q, K, V, O, lse, dO, q_start, k_start=No
     Tq, Tk, Hq, Hkv, D, n = shape.q_tokens, shape.k_tokens, shape.q_heads, shape.kv_heads, shape.head_dim, shape.sequences
     dev, bf16 = _device(Q, "Q"), torch.bfloat16
     q, k, v = _rows_at(Q, dev, Tq, Hq, D, "Q"), _rows_at(K, dev, Tk, Hkv, D, "K"), _rows_at(V, dev, Tk, Hkv, D, "V")
-    dQ = torch.empty((Tq, Hq, D), dtype=bf16, device=Q.device) if dQ is None else dQ
-    dK = torch.empty((Tk, Hkv, D), dtype=bf16, device=Q.device) if dK is None else dK
-    dV = torch.empty((Tk, Hkv, D), dtype=bf16, device=Q.device) if dV is None else dV
+    dQ = _like(Q) if dQ is None else dQ
+    dK = _like(K) if dK is None else dK
+    dV = _like(V) if dV is None else dV
     ws, ws_ptr, ws_bytes = _scratch(prompt_workspace_bytes(shape, PROMPT_ATTN_BWD, causal), workspace, Q, dev)
     _run(dev, "adaspark_prompt_attn_bwd", _prompts_c(shape, q[1], k[1], v[1]), q[0], k[0], v[0], _at(O, dev, bf16, Tq * Hq * D, "O"),
          _at(lse, dev, torch.float32, Tq * Hq, "lse"), _at(dO, dev, bf16, Tq * Hq * D, "dO"),
@@ -732,12 +735,13 @@ def decode_attn(shape: CacheShape, Q, cache: Cache, table, lengths, O=None, lse=
     O bf16 [sequences, Hq, D] (and lse fp32 [sequences, Hq])."""
     rows, D, dev = shape.sequences * shape.q_heads, shape.head_dim, _device(Q, "Q")
     held, pages = _cache_at(shape, cache, table, dev)
+    q_ptr = _at(Q, dev, torch.bfloat16, rows * D, "Q")
     if O is None:
-        O = torch.empty((shape.sequences, shape.q_heads, D), dtype=torch.bfloat16, device=Q.device)
+        O = torch.empty_like(Q) if Q.dim() == 3 else Q.new_empty((shape.sequences, shape.q_heads, D))
     if lse is None and return_lse:
         lse = torch.empty((shape.sequences, shape.q_heads), dtype=torch.float32, device=Q.device)
     ws, ws_ptr, ws_bytes = _scratch(decode_workspace_bytes(shape), workspace, Q, dev)
-    _run(dev, "adaspark_decode_attn", _cache_c(shape), _at(Q, dev, torch.bfloat16, rows * D, "Q"), pages,
+    _run(dev, "adaspark_decode_attn", _cache_c(shape), q_ptr, pages,
          _at(lengths, dev, torch.int32, shape.sequences, "lengths"), *held, _at(O, dev, torch.bfloat16, rows * D, "O"),
          None if lse is None else _at(lse, dev, torch.float32, rows, "lse"), ws_ptr, ws_bytes)
     return (O, lse) if return_lse else O
