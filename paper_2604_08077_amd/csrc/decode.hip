@@ -53,16 +53,21 @@ struct DecodePart {
     int item0;           // number of the sequence's first part
     int key0, key1;
 };
-__host__ __device__ inline int decode_unit(const CacheGeom &g)  // keys of two tiles for each wavefront
+// Keys of the shortest part: two tiles for each wavefront, or, where the sequences alone fill the chip, sixteen: a workgroup's plan, first loads and
+// end take as long as several tiles.  (us with two, with sixteen: 256 sequences of 500 keys, 28/4 heads of 128, bf16 66, 53, 8 bits 53, 40; 200 of
+// 1,000, 32/8 heads 178, 168 and 122, 104; 64 of 1,500 82, 87 and 45, 38; 128 of up to 8,000 386, 390 and 223, 225.)
+__host__ __device__ inline int decode_rows(const CacheGeom &g) { return g.Hkv * ((g.G + 15) / 16); }  // workgroups that a part of a sequence has
+__host__ __device__ inline int decode_unit(const CacheGeom &g)
 {
-    return 2 * decode_waves(g.e4m3) * decode_tile(g.e4m3) / (g.D * (g.e4m3 ? 1 : 2));
+    const int tiles = (long long)g.B * decode_rows(g) >= DECODE_PLACES ? 16 : 2;
+    return tiles * decode_waves(g.e4m3) * decode_tile(g.e4m3) / (g.D * (g.e4m3 ? 1 : 2));
 }
 
 // Parts that a KV head and 16 query heads of its group get: a workgroup each, whole rounds of the chip, at least two for
 // a sequence on average -- the parts have one length, and lengths differ.
 __host__ __device__ inline int decode_parts(const CacheGeom &g)
 {
-    const long long rows = (long long)g.Hkv * ((g.G + 15) / 16);
+    const long long rows = decode_rows(g);
     if (g.B > DECODE_PLAN_SEQS) return g.B;
     const long long slots = (2 * g.B * rows + DECODE_PLACES - 1) / DECODE_PLACES * DECODE_PLACES;
     return (int)(slots / rows > g.B ? slots / rows : g.B);
@@ -190,7 +195,7 @@ __global__ __launch_bounds__(64 * decode_waves(E4M3), 2) void decode_attn_kernel
     const int lane = threadIdx.x & 63, n16 = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-    const int groups = (g.G + 15) / 16, heads = g.Hkv * groups;
+    const int groups = (g.G + 15) / 16, heads = decode_rows(g);
     const int item = (int)(blockIdx.x / (unsigned)heads), hh = (int)(blockIdx.x % (unsigned)heads);
     const int kv = hh / groups, head0 = kv * g.G + hh % groups * 16, nheads = min(16, (kv + 1) * g.G - head0);
     const DecodePart p = decode_plan(g, lengths, item);
@@ -411,7 +416,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(CacheGeom g, const int
     const int s = row / g.Hq, a = row - s * g.Hq;
     struct { int item0, parts; } p = {plan[s].x, plan[s].y};
     if (p.parts <= 1) return;
-    const int groups = (g.G + 15) / 16, heads = g.Hkv * groups;
+    const int groups = (g.G + 15) / 16, heads = decode_rows(g);
     const int kv = a / g.G, hh = kv * groups + (a - kv * g.G) / 16, col = (a - kv * g.G) & 15;
     const float *from = parts + ((size_t)p.item0 * heads + hh) * decode_part_floats(D);
     const size_t step = (size_t)heads * decode_part_floats(D);
@@ -473,7 +478,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(CacheGeom g, const int
 size_t decode_workspace_bytes(const CacheGeom &g)
 {
     const int parts = decode_parts(g);
-    return parts > g.B ? decode_plan_bytes(g) + (size_t)parts * g.Hkv * ((g.G + 15) / 16) * decode_part_floats(g.D) * 4 : 0;
+    return parts > g.B ? decode_plan_bytes(g) + (size_t)parts * decode_rows(g) * decode_part_floats(g.D) * 4 : 0;
 }
 
 template <int D, bool E4M3>
@@ -487,7 +492,7 @@ static hipError_t launch_decode(const CacheGeom &g, const uint16_t *Q, const int
     const bool shared = decode_parts(g) > g.B;
     int2 *plan = shared ? static_cast<int2 *>(ws) : nullptr;
     float *parts = shared ? reinterpret_cast<float *>(static_cast<char *>(ws) + decode_plan_bytes(g)) : nullptr;
-    const unsigned heads = (unsigned)(g.Hkv * ((g.G + 15) / 16));
+    const unsigned heads = (unsigned)decode_rows(g);
     hipLaunchKernelGGL((decode_attn_kernel<D, E4M3>), dim3((unsigned)decode_parts(g) * heads), dim3(C::THREADS), C::BYTES, st, g, Q,
                        table, lengths, static_cast<const unsigned char *>(c.K), static_cast<const unsigned char *>(c.V), c.ks,
                        c.vs, O, lse, plan, parts);
