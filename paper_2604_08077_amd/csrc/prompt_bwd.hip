@@ -178,7 +178,8 @@ __device__ __forceinline__ void early_delta(const PromptGeom &g, int s, int kv, 
     }
 }
 
-// Start values of every row: 256 / (D / 8) rows to a workgroup, D / 8 lanes to a row.  A row without keys (log-sum-exp -inf) gets
+constexpr int PREP_DEPTH = 4;  // rows that a lane works on at once
+// Start values of every row: PREP_DEPTH times 256 / (D / 8) rows to a workgroup, D / 8 lanes to a row.  A row without keys (log-sum-exp -inf) gets
 // no part in anything.  The first B * Hkv workgroups leave the mean keys, a thread to a column of some of the keys, the
 // very first wavefront also the length of a span; the next B * Hkv * early on the rows with few keys.
 template <int D>
@@ -227,36 +228,57 @@ __global__ __launch_bounds__(256, 4) void prompt_prep_kernel(PromptGeom g, int m
                        lse, delta);
         return;
     }
-    const long long r = ((long long)(blockIdx.x - skip) * 256 + threadIdx.x) / CPR;
-    const int col = threadIdx.x % CPR, lane = threadIdx.x & 63;
-    float part = 0.f;
-    if (r < rows) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8 *>(dO + r * D + col * 8), b = *reinterpret_cast<const bf16x8 *>(O + r * D + col * 8);
+    constexpr int RPW = 64 / CPR;  // rows of a wavefront at a time, and as many PREP_DEPTH times over
+    const int lane = threadIdx.x & 63, col = lane % CPR, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long row0 = ((long long)(blockIdx.x - skip) * 4 + wave) * (RPW * PREP_DEPTH);
+    if (row0 > rows) return;
+    bf16x8 a[PREP_DEPTH], b[PREP_DEPTH];
+    float l[PREP_DEPTH];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) part = fmaf((float)a[e], (float)b[e], part);
-    }
-#pragma unroll
-    for (int d = CPR / 2; d >= 1; d >>= 1) part += __shfl_xor(part, d, 64);
-    // the row's sequence: the last one with a start at or before its token
-    const int tok = (int)((unsigned)min(r, rows) / (unsigned)g.Hq);
-    int seq = 0;
-    for (int s = 0; s < g.B; s += 64) {
-        const int start = g.q_start[min(s + lane, g.B - 1)];
-        unsigned long long last = 0ull;
-#pragma unroll
-        for (int j = 0; j < 64 / CPR; ++j) {
-            last = __ballot(s + lane < g.B && start <= __builtin_amdgcn_readlane(tok, j * CPR));
-            if (lane / CPR == j && last != 0ull) seq = s + 63 - __clzll(last);
+    for (int u = 0; u < PREP_DEPTH; ++u) {
+        const long long r = max(0ll, min(row0 + u * RPW + lane / CPR, rows - 1));
+        if (rows > 0) {
+            a[u] = *reinterpret_cast<const bf16x8 *>(dO + r * D + col * 8);
+            b[u] = *reinterpret_cast<const bf16x8 *>(O + r * D + col * 8);
+            l[u] = lse[r];
         }
-        if (last != ~0ull) break;  // (the wavefront's last row has the last of their sequences)
     }
-    if (col != 0 || r > rows) return;
-    const float l = r < rows ? lse[r] : -INFINITY;
-    lse2[r] = l == -INFINITY ? -INFINITY : -l * sqrtf((float)D);  // = -(lse in base 2) / (softmax scale in base 2)
-    const PromptSeq p = prompt_seq(g, seq);
-    int from, to;
-    few_keys_of(g, p.n, p.m, from, to);
-    if (r == rows || tok - p.q0 < from || tok - p.q0 >= to) delta[r] = -part;
+    // which of the wavefront's tokens, t0 .. t1, have few keys: sequences 64 at a time, from those on that hold t0
+    const int t0 = (int)((unsigned)row0 / (unsigned)g.Hq), t1 = (int)((unsigned)min(row0 + RPW * PREP_DEPTH - 1, rows) / (unsigned)g.Hq);
+    static_assert(RPW * PREP_DEPTH <= 64, "a bit for each token");
+    unsigned long long few = 0ull;
+    int s = 0;
+    for (int hi = (g.B + 63) >> 6; hi - s > 1;) {
+        const int mid = (s + hi) >> 1;
+        if (g.q_start[64 * mid] <= t0) s = mid;
+        else hi = mid;
+    }
+    s *= 64;
+    do {
+        int from = 0, to = 0;
+        if (s + lane < g.B) {
+            const PromptSeq p = prompt_seq(g, s + lane);
+            few_keys_of(g, p.n, p.m, from, to);
+            from += p.q0;
+            to += p.q0;
+        }
+        for (int t = t0; t <= t1; ++t)
+            if (__ballot(from <= t && t < to) != 0ull) few |= 1ull << (t - t0);
+        s += 64;
+    } while (s < g.B && g.q_start[s] <= t1);
+#pragma unroll
+    for (int u = 0; u < PREP_DEPTH; ++u) {
+        const long long r = row0 + u * RPW + lane / CPR;
+        float part = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) part = fmaf((float)a[u][e], (float)b[u][e], part);
+#pragma unroll
+        for (int d = CPR / 2; d >= 1; d >>= 1) part += __shfl_xor(part, d, 64);
+        if (col != 0 || r > rows) continue;
+        lse2[r] = r == rows || l[u] == -INFINITY ? -INFINITY : -l[u] * sqrtf((float)D);  // = -(lse in base 2) / (softmax scale in base 2)
+        if (r == rows) delta[r] = 0.f;
+        else if (((few >> ((int)((unsigned)r / (unsigned)g.Hq) - t0)) & 1ull) == 0ull) delta[r] = -part;
+    }
 }
 
 struct PromptBwdArgs {
@@ -818,7 +840,7 @@ static hipError_t launch_bwd(const PromptGeom &g, const uint16_t *Q, const uint1
     const PromptSpans spans = prompt_spans(g);
     const PromptCut cut = prompt_cut(g, PB_BLOCK, D);
     const PromptBwdArgs arg{Q, K, V, dO, w.lse2, w.delta, w.mean, w.span, w.part, dQ, dK, dV};
-    const long long rows = (long long)g.Tq * g.Hq, per = 256 / (D / 8);
+    const long long rows = (long long)g.Tq * g.Hq, per = PREP_DEPTH * 256 / (D / 8);
     const int early = early_groups(g);
     hipLaunchKernelGGL((prompt_prep_kernel<D>), dim3((unsigned)((long long)g.B * g.Hkv * (1 + early) + (rows + 1 + per - 1) / per)), dim3(256), 0, st, g,
                        spans.most, early, w.span, Q, K, V, w.mean, rows, O, dO, lse, w.lse2, w.delta);

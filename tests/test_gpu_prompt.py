@@ -82,6 +82,7 @@ def test_forward_and_gradients(B, heads, case, causal):
     ((8, 8, 64), [3, 40], [9000, 5000], 1.0),  # keys shared out to many workgroups
     ((6, 2, 128), [500], None, 4.0),           # scores in the hundreds
     ((4, 2, 64), [1] * 600, [3] * 600, 1.0),   # more sequences than a wavefront holds at once
+    ((2, 1, 128), [i * i % 97 for i in range(150)], [i * i % 97 + i % 3 for i in range(150)], 1.0),  # rows of few and of more keys in turn
 ])
 def test_long_and_large(B, heads, q_len, k_len, scale):
     k_len = k_len or q_len
