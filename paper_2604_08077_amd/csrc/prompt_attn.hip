@@ -125,6 +125,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptGeom g, Promp
     if (ntiles > 0) {
         issue_k(0, 0);
         issue_v(0, 0);
+        if (ntiles > 1) issue_k(1, 1);
     }
 
     // the wavefront's rows (past the last one it is repeated)
@@ -158,11 +159,12 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptGeom g, Promp
         for (int e = 0; e < DT; ++e) oacc[s][e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // Slot t works on K(t) and V(t-1); K(t+1) and V(t) are started when it opens, and waited for at the next.
+    // Slot t works on K(t) and V(t-1); K(t+1) and V(t) are started when it opens (those of slot 0 with the first tiles), and waited for at the next.
     int kst = 0;  // stage of K(t); V(t-1) sits in the other
     auto open_slot = [&](int t) __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        if (t > 0 && t < ntiles) issue_v(t, kst);
+        if (t == 0) return;
+        if (t < ntiles) issue_v(t, kst);
         if (t + 1 < ntiles) issue_k(t + 1, kst ^ 1);
     };
     auto next_slot = [&](int t) __attribute__((always_inline)) {

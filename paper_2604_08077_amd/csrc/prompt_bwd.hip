@@ -25,7 +25,7 @@
 // workspace; prompt_bwd_join_kernel adds them in their order.  Walks of few row blocks are shared out as in the forward (prompt.h).
 //
 // Workgroups of four wavefronts and two stages, two to a CU, which are not in step; eight wavefronts and three stages take 1.05 times as long (a
-// training pass over 16k tokens in 5 sequences of 28/4 heads of 128: 2.01 ms, 870 TF/s).
+// training pass over 16k tokens in 5 sequences of 28/4 heads of 128: 2.00 ms, 875 TF/s).
 #include <algorithm>
 
 #include "prompt.h"
