@@ -459,9 +459,10 @@ __device__ __forceinline__ void prompt_dq(const PromptGeom &g, const PromptCut &
     static_assert(KSTEPS % 2 == 0 && DT % 2 == 0, "the operands' two places take turns");
 
     if (first < ntiles) issue(first, first & 1);
+    if (first + 1 < ntiles) issue(first + 1, (first + 1) & 1);
     for (int t = first; t < ntiles; ++t) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (t + 1 < ntiles) issue(t + 1, (t + 1) & 1);  // (the stage read last at tile t - 1)
+        if (t > first && t + 1 < ntiles) issue(t + 1, (t + 1) & 1);  // (the stage read last at tile t - 1)
         if (t < mine) work(t, t & 1);
     }
     const float c = 1.0f / sqrtf((float)D);
@@ -716,10 +717,11 @@ __device__ __forceinline__ void prompt_dkv(const PromptGeom &g, int per_head, co
     };
 
     if (ntiles > 0) issue(0, 0);
+    if (ntiles > 1) issue(1, 1);
     int t = 0;
     auto tile = [&](auto edge_tag) __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // everybody's loads of the tile have landed
-        if (t + 1 < ntiles) issue(t + 1, (t + 1) & 1);  // (the stage read last at tile t - 1)
+        if (t > 0 && t + 1 < ntiles) issue(t + 1, (t + 1) & 1);  // (the stage read last at tile t - 1)
         const int r0 = row0 + 64 * t;
         if (busy && (!decltype(edge_tag)::value || r0 + 63 >= mine_from)) work(t & 1, r0, edge_tag);
         ++t;
