@@ -374,7 +374,8 @@ int adaspark_ffn_sparse(const adaspark_shape *shape, const adaspark_ffn_dims *di
  *   O          out  bf16 [q_tokens][q_heads][head_dim], contiguous
  *   lse        out  fp32 [q_tokens][q_heads] natural-log sum-exp of the scaled logits, or NULL
  *   workspace       adaspark_prompt_workspace_bytes(ADASPARK_PROMPT_ATTN): 0 unless there are so few rows that each row's keys are
- *                   shared out to several workgroups; may then be NULL
+ *                   shared out to several workgroups; may then be NULL.  Calls that may overlap in time, replays of two graphs too, need a
+ *                   workspace each, here as for the calls below
  * Score products are exact in fp32 and the log-sum-exp is that of fp32 weights; the weights are rounded to bf16 (off by up to 2^-8 of each) for their
  * products with V.  K and V of a sequence have to be finite: a row may multiply the V of a key that it does not attend by a weight of 0.
  * Outputs must not overlap inputs or each other (ADASPARK_EINVAL).

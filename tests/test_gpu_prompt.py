@@ -303,3 +303,17 @@ def test_calls_at_once(B):
         torch.cuda.synchronize()
         for x, y in zip(alone, got):
             assert all(torch.equal(a, b) for a, b in zip(x, y))
+
+
+@pytest.mark.parametrize("q_len,k_len", [([0, 0], [5, 700]), ([3, 200], [0, 0]), ([0, 300, 0], [0, 0, 9])])
+@pytest.mark.parametrize("causal", [True, False])
+def test_nothing_to_attend(B, q_len, k_len, causal):
+    heads, tq, tk = (6, 2, 128), sum(q_len), sum(k_len)
+    Q, K, V, dO = inputs(heads, tq, tk, 3)
+    sh = B.PromptShape(len(q_len), tq, tk, *heads)
+    qs, ks = R.starts(q_len).cuda(), R.starts(k_len).cuda()
+    O, lse = B.prompt_attn(sh, Q, K, V, qs, ks, causal=causal, return_lse=True)
+    assert not O.any() and torch.isneginf(lse).all()
+    out = [torch.full_like(t, 7) for t in (Q, K, V)]
+    B.prompt_attn_bwd(sh, Q, K, V, O, lse, dO, qs, ks, causal=causal, dQ=out[0], dK=out[1], dV=out[2])
+    assert not any(t.any() for t in out)
