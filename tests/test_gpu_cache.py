@@ -299,3 +299,27 @@ def test_a_replayed_step(B, fmt):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(O, eager[i])
+
+
+def test_arguments_that_are_refused(B):
+    heads, length = (4, 2, 64), 20
+    sh, cache, table, lengths = make(B, heads, [length], 16, "e4m3", 2)
+    K, V = tokens(heads, length, 1)
+    start = R.starts([length]).cuda()
+    q = torch.zeros(1, 4, 64, dtype=torch.bfloat16, device="cuda")
+    write = dict(shape=sh, K=K, V=V, start=start, cache=cache, table=table, lengths=lengths)
+    for bad in (dict(K=K.float()), dict(V=V[:-1]), dict(start=start.long()), dict(table=table[:, :-1]), dict(lengths=lengths.cpu()),
+                dict(cache=cache._replace(k_scale=None)), dict(cache=cache._replace(K=cache.K[:-1])), dict(shape=sh._replace(format="int8"))):
+        with pytest.raises(ValueError):
+            B.cache_write(**{**write, **bad})
+    with pytest.raises(ValueError):
+        B.cache_read(sh, cache, table, start, length, K=K[:-1])
+    with pytest.raises(B.AdasparkError):
+        B.cache_read(sh, cache, table, start, length, K=K, V=K)
+    for bad in (dict(Q=q.float()), dict(Q=q.expand(2, 4, 64)), dict(table=table.long()), dict(lse=torch.zeros(4, dtype=torch.float64, device="cuda"))):
+        with pytest.raises(ValueError):
+            B.decode_attn(**{**dict(shape=sh, Q=q, cache=cache, table=table, lengths=lengths), **bad})
+    with pytest.raises(B.AdasparkError):
+        B.decode_attn(sh, q, cache, table, lengths, O=q)
+    with pytest.raises(B.AdasparkError):
+        B.decode_attn(sh, q, cache, table, lengths, workspace=torch.zeros(16, dtype=torch.uint8, device="cuda"))

@@ -317,3 +317,26 @@ def test_nothing_to_attend(B, q_len, k_len, causal):
     out = [torch.full_like(t, 7) for t in (Q, K, V)]
     B.prompt_attn_bwd(sh, Q, K, V, O, lse, dO, qs, ks, causal=causal, dQ=out[0], dK=out[1], dV=out[2])
     assert not any(t.any() for t in out)
+
+
+def test_arguments_that_are_refused(B):
+    heads, n = (4, 2, 64), 9
+    Q, K, V, dO = inputs(heads, n, n, 1)
+    sh, start = B.PromptShape(1, n, n, *heads), R.starts([n]).cuda()
+    O, lse = B.prompt_attn(sh, Q, K, V, start, return_lse=True)
+    wide = torch.zeros(n, 2, 128, dtype=torch.bfloat16, device="cuda")
+    for bad in (dict(Q=Q.float()), dict(Q=Q[:-1]), dict(K=K.cpu()), dict(V=wide[..., :64]), dict(q_start=start.long()), dict(k_start=start[:1]),
+                dict(O=O.float()), dict(lse=lse[:, :2]), dict(workspace=torch.zeros(64, device="cuda")), dict(K=K.transpose(1, 2).contiguous())):
+        with pytest.raises(ValueError):
+            B.prompt_attn(**{**dict(shape=sh, Q=Q, K=K, V=V, q_start=start), **bad})
+    with pytest.raises(B.AdasparkError):
+        B.prompt_attn(sh, Q, K, V, start, O=Q)
+    with pytest.raises(B.AdasparkError):  # a stride that is no multiple of eight elements
+        B.prompt_attn(sh, Q, torch.zeros(n * 132, dtype=torch.bfloat16, device="cuda").as_strided((n, 2, 64), (132, 64, 1)), V, start)
+    for bad in (dict(dO=dO[:, :2]), dict(O=O.float()), dict(lse=lse.half()), dict(dK=Q), dict(dO=dO.transpose(0, 1))):
+        with pytest.raises(ValueError):
+            B.prompt_attn_bwd(**{**dict(shape=sh, Q=Q, K=K, V=V, O=O, lse=lse, dO=dO, q_start=start), **bad})
+    with pytest.raises(B.AdasparkError):
+        B.prompt_attn_bwd(sh, Q, K, V, O, lse, dO, start, dQ=dO)
+    with pytest.raises(B.AdasparkError):
+        B.prompt_attn_bwd(sh, Q, K, V, O, lse, dO, start, workspace=torch.zeros(16, dtype=torch.uint8, device="cuda"))
